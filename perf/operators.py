@@ -188,7 +188,7 @@ def _quantise(u, bits):
         z = z.view(torch.float32) - (y < 1).float()
         code = (z >= 0.5).int() + (z >= 1) + (z >= 1.5) + (z >= 2) + (z >= 3) + (z >= 4) + (z >= 6)
     code = code + torch.signbit(x) * 8
-    fine = torch.isfinite(most)
+    fine = most <= 6 * 2.0 ** 125  # what is above, an infinity or a NaN makes the block read as NaN
     code = torch.where(fine[..., None], code, torch.zeros_like(code))
     return code.to(torch.uint8).reshape(n, -1), torch.where(fine, byte, torch.full_like(byte, 255)).to(torch.uint8)
 
