@@ -250,6 +250,76 @@ int32_t hadfl_last_round_pack(const hadfl_handle *h);
  * launch or no fused round has run.  Synchronises the stream. */
 int hadfl_stats_read_round(hadfl_handle *h, int32_t back, float *out_norm2, float *out_div2);
 
+/* ---- exchange in messages of 4 bits per parameter ------------------------------------------------
+ * What devices send each other in a synchronisation is, in the paper, the whole model at storage precision
+ * (its volume is the method's cost).  These calls send updates instead, in microscaled 4-bit floating point
+ * (not in the paper): 4.25 bits per parameter.
+ *
+ * The message of one device: u, the P values to send, in blocks of 32 consecutive parameters (the last one
+ * filled up with zeros).  A block has a scale 2^(b - 127), b a byte, and 32 codes of 4 bits: a sign and one
+ * of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (code 0 to 7, +8 if negative); a parameter reads as code value * scale, in
+ * fp32.  b is the smallest byte whose scale has max|u| <= 6 * scale, so that no value is cut off.  A block with
+ * an infinity, a NaN or a magnitude above 6 * 2^125 (2.55e38) gets b = 255 and codes 0, and reads as 32 NaNs.
+ * Codes are rounded to the nearest value (ties to the even code), or stochastically: up with probability
+ * (way from the lower value) / (distance of the two), in steps of 2^-16, so that a message is right on
+ * average.  The 16 random bits of parameter p of device i come from the Philox4x32-10 block with key = the
+ * handle's seed and counter (p / 8, round mod 2^32, i, 'Q' << 24 | round >> 32): word (p mod 8) / 2, low
+ * half for even p, high half for odd ones.  They are added to the upper 16 of the 22 low mantissa bits
+ * of t (t = |u| / scale, or fl(t + 1) where t < 1), those 22 bits are dropped, and the 1 is taken off again.
+ * In memory: ceil(P / 32) * 16 bytes of codes (two per byte, the even parameter in the low half), zeros up to
+ * hadfl_packed_scales_at (a multiple of 128), ceil(P / 32) scale bytes, zeros up to hadfl_packed_bytes (a
+ * multiple of 128).  hadfl_pack writes all of these bytes.
+ *
+ * Arguments of the calls below:
+ *   messages  DEVICE pointer, 16-byte aligned, to N messages: device i's at i * hadfl_packed_bytes(P) bytes.
+ *   base      DEVICE pointer, 16-byte aligned, to P values in the parameters' storage type that all
+ *             devices have in common (such as the last model that was sent to all of them), or NULL for
+ *             zeros.  It may be a row of the parameter arena.
+ *   residual  DEVICE pointer, 16-byte aligned, to N rows of hadfl_row_stride floats, or NULL: what earlier
+ *             messages of each device have left out (zeros at first).  It is added to the next update
+ *             and takes what that message leaves out.
+ * They are memory of the handle's device, used on the handle's stream, and stay the caller's.  NULL where it
+ * is not allowed, a misaligned pointer, memory of the host or of another device, and buffers that overlap
+ * each other or the arenas (a base that is a row of parameters excepted) give HADFL_ERR_INVALID.
+ * Versions and step counters change in hadfl_aggregate_packed only.  All calls are asynchronous, allocate
+ * nothing and can be captured in a graph. */
+
+/* Bytes of the message of n_params parameters, and the offset of its scales; 0 for n_params < 1 or above
+ * 2^34 - 4.  Host only. */
+int64_t hadfl_packed_bytes(int64_t n_params);
+int64_t hadfl_packed_scales_at(int64_t n_params);
+
+/* Writes the messages of the n devices device_ids (distinct): u = (w[i] - base) + residual[i] (each operation
+ * rounded to fp32; what is NULL is left out), and residual[i] = u - (the message as it reads), 0 in blocks
+ * that read as NaN.  The parameters are not touched.  rounding: HADFL_ROUND_* of the codes; round:
+ * 0 .. 2^56 - 1, names the random numbers (with HADFL_ROUND_NEAREST it is not used).  One kernel:
+ * reads w and writes the message, and reads and writes the residual; the base is read once for all devices. */
+int hadfl_pack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const void *base, float *residual,
+               int32_t rounding, int64_t round, void *messages);
+
+/* The parameters of the n devices device_ids (distinct) become what their messages say:
+ * w[i] = base + message i (rounded to fp32, then to nearest even in bf16 storage; only the message if base is NULL).
+ * For a receiver that holds the senders' models, such as a coordinator with an arena of its own.  One kernel. */
+int hadfl_unpack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const void *base, const void *messages);
+
+/* Partial aggregation, Eq. 5, from the messages of the k devices `selected` (distinct, in this order):
+ *     acc = a_0 * d_0;  acc = fma(a_j, d_j, acc), j = 1..k-1;  w[dst_ids[i]] = base + acc for all i
+ * d_j the message of selected[j], a_j as in hadfl_aggregate (from `versions`, NULL = the handle's counters).
+ * dst_ids: the n receivers (distinct); n = 0 and dst_ids = NULL: the selected devices.  move_base != 0: the
+ * base becomes the aggregate too (base must not be NULL), as it may when all devices receive it.  Momentum is
+ * not touched.  Every receiver takes the largest version among the selected devices.  One kernel. */
+int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, const double *versions, void *base,
+                           int32_t move_base, const int32_t *dst_ids, int32_t n, const void *messages);
+
+/* Scalar products of messages: out[i * n + j] = sum over all parameters p of a_ids[i]'s message in a_messages
+ * times b_ids[j]'s in b_messages, 1 <= m, n <= N, ids in [0, N) in any order, also repeated.  b_ids = NULL and b_messages
+ * = NULL (n = 0): the second set is the first, and out the m x m matrix of its products, which gives the norm of
+ * every update and the angle and distance of every two (hadfl_stats: the distances to one replica).
+ * out: DEVICE pointer to floats, 4-byte aligned.  A message with a block that reads as NaN has NaN products.
+ * Deterministic: fixed grid and summation order. */
+int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const void *a_messages, const int32_t *b_ids,
+                      int32_t n, const void *b_messages, float *out);
+
 /* Per-replica statistics (not in the paper; diagnostics of how far the replicas have drifted):
  * out_norm2[i] = sum_p w_i[p]^2, out_div2[i] = sum_p (w_i[p] - w_ref[p])^2, N floats each.
  * Deterministic: fixed grid, fixed summation order, fp32 within a chunk, fp64 above.

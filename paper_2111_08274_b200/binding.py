@@ -75,6 +75,13 @@ SIGNATURES = {
     "hadfl_round": (C.c_int, [_H, _i32p, _i32p, C.c_int32, C.c_float, C.c_int64, _f64p, C.c_uint64, C.c_int32,
                               C.c_int32, _i32p]),
     "hadfl_rounds": (C.c_int, [_H, C.c_int64, C.c_int32, _i32p, C.c_float, C.c_uint64, C.c_int32, C.c_int32, _i32p]),
+    "hadfl_packed_bytes": (C.c_int64, [C.c_int64]),
+    "hadfl_packed_scales_at": (C.c_int64, [C.c_int64]),
+    "hadfl_pack": (C.c_int, [_H, _i32p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]),
+    "hadfl_unpack": (C.c_int, [_H, _i32p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "hadfl_aggregate_packed": (C.c_int, [_H, _i32p, C.c_int32, _f64p, C.c_void_p, C.c_int32, _i32p, C.c_int32,
+                                         C.c_void_p]),
+    "hadfl_packed_dots": (C.c_int, [_H, _i32p, C.c_int32, C.c_void_p, _i32p, C.c_int32, C.c_void_p, C.c_void_p]),
     "hadfl_stats_enqueue": (C.c_int, [_H, C.c_int32]),
     "hadfl_stats_read": (C.c_int, [_H, _f32p, _f32p]),
     "hadfl_stats": (C.c_int, [_H, C.c_int32, _f32p, _f32p]),
@@ -176,6 +183,16 @@ def hadfl_stats_noalloc(w_ptr, dtype, n_devices, n_params, row_stride_elems, ref
     (see include/hadfl.h).  out_stats_ptr: 2N device floats, norm2 then div2.  Asynchronous."""
     return int(lib().hadfl_stats_noalloc(w_ptr, dtype, n_devices, n_params, row_stride_elems,
                                          ref_device, out_stats_ptr, stream or None))
+
+
+def hadfl_packed_bytes(n_params):
+    """Bytes of the message of n_params parameters (host only)."""
+    return int(lib().hadfl_packed_bytes(n_params))
+
+
+def hadfl_packed_scales_at(n_params):
+    """Byte offset of the scales in that message (host only)."""
+    return int(lib().hadfl_packed_scales_at(n_params))
 
 
 def hadfl_debug_build():
@@ -292,6 +309,32 @@ class Hadfl:
         dst = _arr(dst_ids, np.int32)
         self._check(self._lib.hadfl_integrate(self._h, src, _p(dst, C.c_int32), len(dst), beta),
                     "hadfl_integrate")
+
+    def pack(self, device_ids, messages_ptr, base_ptr=None, residual_ptr=None, rounding=ROUND_NEAREST, round_=0):
+        """Pointers here and in the calls below: device addresses, e.g. a torch tensor's data_ptr()."""
+        ids = _arr(device_ids, np.int32)
+        self._check(self._lib.hadfl_pack(self._h, _p(ids, C.c_int32), len(ids), base_ptr, residual_ptr, rounding,
+                                         round_, messages_ptr), "hadfl_pack")
+
+    def unpack(self, device_ids, messages_ptr, base_ptr=None):
+        ids = _arr(device_ids, np.int32)
+        self._check(self._lib.hadfl_unpack(self._h, _p(ids, C.c_int32), len(ids), base_ptr, messages_ptr),
+                    "hadfl_unpack")
+
+    def aggregate_packed(self, selected, messages_ptr, base_ptr=None, dst_ids=None, move_base=False, versions=None):
+        """dst_ids: the receivers (None: the selected devices)."""
+        sel, dst, v = _arr(selected, np.int32), _arr(dst_ids, np.int32), _arr(versions, np.float64)
+        self._check(self._lib.hadfl_aggregate_packed(self._h, _p(sel, C.c_int32), len(sel), _p(v, C.c_double), base_ptr,
+                                                     1 if move_base else 0, _p(dst, C.c_int32),
+                                                     0 if dst is None else len(dst), messages_ptr),
+                    "hadfl_aggregate_packed")
+
+    def packed_dots(self, a_ids, a_messages_ptr, out_ptr, b_ids=None, b_messages_ptr=None):
+        """out_ptr: len(a_ids) x len(b_ids) device floats (b_ids None: the first set with itself)."""
+        a, b = _arr(a_ids, np.int32), _arr(b_ids, np.int32)
+        self._check(self._lib.hadfl_packed_dots(self._h, _p(a, C.c_int32), len(a), a_messages_ptr, _p(b, C.c_int32),
+                                                0 if b is None else len(b), b_messages_ptr, out_ptr),
+                    "hadfl_packed_dots")
 
     def set_sync_beta(self, beta):
         self._check(self._lib.hadfl_set_sync_beta(self._h, beta), "hadfl_set_sync_beta")

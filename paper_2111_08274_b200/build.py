@@ -12,8 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhadfl.so")
 LIB_DEBUG = os.path.join(HERE, "libhadfl_debug.so")   # -DHADFL_DEBUG: bounds-checked kernels
-SOURCES = ["hadfl.cu", "selection.cpp"]
-DEPS = SOURCES + ["kernels.cuh", "philox.cuh", "debug_check.cuh", "selection.h",
+SOURCES = ["hadfl.cu", "packed.cu", "selection.cpp"]
+DEPS = SOURCES + ["kernels.cuh", "storage.cuh", "packed.cuh", "packed.h", "philox.cuh", "debug_check.cuh", "selection.h",
                   os.path.join("..", "..", "include", "hadfl.h")]
 
 

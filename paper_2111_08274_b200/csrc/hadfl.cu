@@ -13,10 +13,12 @@
 #include <vector>
 
 #include "kernels.cuh"
+#include "packed.h"
 #include "selection.h"
 
 using namespace hadfl;
 
+constexpr int64_t kMaxParams = ((int64_t)1 << 34) - 4;
 constexpr int kStatsWatch = 4;  // one call of 32 rounds, or a few rounds as separate calls
 
 struct hadfl_handle {
@@ -66,6 +68,7 @@ struct hadfl_handle {
   int round_batch = kRoundBatchMax;  // most rounds that hadfl_rounds puts into one launch (1: never batch)
   int last_launch_rounds = 0;        // rounds in the most recent launch of the fused round kernel
   int last_launch_pack = 0;          // columns per thread in that launch
+  void *d_dots = nullptr;  // products of messages: the blocks' partial sums
   // model backup that overlaps with later rounds: staging row + copy stream
   void *d_backup = nullptr;
   size_t backup_elem = 4;        // bytes per staged parameter: 2 where memory is too short to widen bf16 on the device
@@ -171,7 +174,8 @@ RowStep row_step(const hadfl_handle *h, int dev, uint64_t base, int steps) {
 DebugRanges g_debug_host;
 
 int debug_publish() {
-  return cudaMemcpyToSymbol(g_debug, &g_debug_host, offsetof(DebugRanges, error)) == cudaSuccess ? 0 : 1;
+  const size_t bytes = offsetof(DebugRanges, error);
+  return cudaMemcpyToSymbol(g_debug, &g_debug_host, bytes) == cudaSuccess ? packed_debug_publish(&g_debug_host, bytes) : 1;
 }
 void debug_add(const void *p, size_t nbytes) {
   if (!p || nbytes == 0 || g_debug_host.n >= kDebugRanges) return;
@@ -193,7 +197,22 @@ int debug_error(uint64_t *addr) {
   DebugRanges now;
   if (cudaMemcpyFromSymbol(&now, g_debug, sizeof(now)) != cudaSuccess) return 1;
   if (addr) *addr = now.bad_addr;
-  return now.error ? 1 : 0;
+  return packed_debug_error(addr) || now.error ? 1 : 0;
+}
+// Buffers that callers hand to a call, which may still run when it returns, and again in a captured graph: they stay
+// in the table, the oldest making room.
+int debug_keep(const void *p, size_t nbytes) {
+  static const void *kept[kDebugRanges / 2];
+  static int next = 0;
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  for (int r = 0; r < g_debug_host.n; ++r)
+    if (range_holds(g_debug_host.lo[r], g_debug_host.hi[r], at, nbytes)) return 0;
+  cudaDeviceSynchronize();
+  debug_remove(kept[next]);
+  kept[next] = p;
+  next = (next + 1) % (kDebugRanges / 2);
+  debug_add(p, nbytes);
+  return debug_publish();
 }
 #define HADFL_DEBUG_RESULT()                            \
   do {                                                   \
@@ -766,7 +785,7 @@ int hadfl_init(const hadfl_config *cfg, hadfl_handle **out) {
   if (!cfg || !out) return HADFL_ERR_INVALID;
   *out = nullptr;
   if (cfg->n_devices < 1 || cfg->n_devices > HADFL_MAX_DEVICES) return HADFL_ERR_INVALID;
-  if (cfg->n_params < 1 || cfg->n_params > ((int64_t)1 << 34) - 4) return HADFL_ERR_INVALID;
+  if (cfg->n_params < 1 || cfg->n_params > kMaxParams) return HADFL_ERR_INVALID;
   if (cfg->dtype != HADFL_DTYPE_FP32 && cfg->dtype != HADFL_DTYPE_BF16) return HADFL_ERR_INVALID;
   if (cfg->m_dtype != HADFL_DTYPE_FP32 && cfg->m_dtype != HADFL_DTYPE_BF16) return HADFL_ERR_INVALID;
   if (cfg->rounding != HADFL_ROUND_NEAREST && cfg->rounding != HADFL_ROUND_STOCHASTIC)
@@ -858,6 +877,7 @@ int hadfl_init(const hadfl_config *cfg, hadfl_handle **out) {
   HADFL_CUDA(h, cudaMalloc((void **)&h->d_round_ticket, sizeof(unsigned int) * (1 + n_groups)));
   HADFL_CUDA(h, cudaMemsetAsync(h->d_round_ticket, 0, sizeof(unsigned int) * (1 + n_groups),
                                 h->stream));
+  HADFL_CUDA(h, cudaMalloc(&h->d_dots, packed_dots_scratch_bytes(h->sm_count)));
   HADFL_CUDA(h, cudaMemsetAsync(h->d_ticket, 0, sizeof(unsigned int), h->stream));
 #ifdef HADFL_DEBUG
   debug_add(h->w, elems * elem_size(h));
@@ -867,6 +887,7 @@ int hadfl_init(const hadfl_config *cfg, hadfl_handle **out) {
   debug_add(h->stats_host, stats_bytes);
   debug_add(h->d_round_partials, sizeof(double) * round_vals * (size_t)scratch_grid);
   debug_add(h->d_round_group_partials, sizeof(double) * round_vals * n_groups);
+  debug_add(h->d_dots, packed_dots_scratch_bytes(h->sm_count));
   HADFL_CUDA(h, cudaDeviceSynchronize());
   if (debug_publish()) return HADFL_ERR_CUDA;
 #endif
@@ -888,6 +909,7 @@ int hadfl_destroy(hadfl_handle *h) {
   debug_remove(h->stats_host);
   debug_remove(h->d_round_partials);
   debug_remove(h->d_round_group_partials);
+  debug_remove(h->d_dots);
   debug_publish();
 #endif
   if (h->own_arena) {
@@ -901,6 +923,7 @@ int hadfl_destroy(hadfl_handle *h) {
   cudaFree(h->d_round_partials);
   cudaFree(h->d_round_group_partials);
   cudaFree(h->d_round_ticket);
+  cudaFree(h->d_dots);
   if (h->backup_stream) cudaStreamSynchronize(h->backup_stream);
   cudaFree(h->d_backup);
   if (h->backup_ready) cudaEventDestroy(h->backup_ready);
@@ -1070,6 +1093,164 @@ int hadfl_integrate(hadfl_handle *h, int32_t src, const int32_t *dst_ids, int32_
     if (beta == 1.0f || h->version[src] > v) v = h->version[src];
   }
   return HADFL_OK;
+}
+
+int64_t hadfl_packed_bytes(int64_t n_params) {
+  return n_params < 1 || n_params > kMaxParams ? 0 : packed_bytes(n_params);
+}
+int64_t hadfl_packed_scales_at(int64_t n_params) {
+  return n_params < 1 || n_params > kMaxParams ? 0 : packed_scales_at(n_params);
+}
+
+namespace {
+
+struct ByteRange {
+  uint64_t lo = 0, hi = 0;
+  ByteRange() = default;
+  ByteRange(const void *p, size_t bytes) : lo((uint64_t)(uintptr_t)p), hi((uint64_t)(uintptr_t)p + bytes) {}
+  bool meets(const ByteRange &o) const { return lo < o.hi && o.lo < hi; }
+};
+
+// A buffer of the caller: aligned, and memory of the handle's device (anything else would become a fault in the kernel).
+bool device_buffer(const hadfl_handle *h, const void *p, size_t align) {
+  if (!p || (uintptr_t)p % align) return false;
+  cudaPointerAttributes at;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return (at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged) && at.device == h->device;
+}
+
+// The buffers of an exchange call, as the header says.
+bool exchange_buffers(const hadfl_handle *h, const void *base, const void *residual, const void *messages) {
+  const size_t n = (size_t)h->cfg.n_devices, row = (size_t)h->stride * elem_size(h);
+  if (!device_buffer(h, messages, 16)) return false;
+  if (base && !device_buffer(h, base, 16)) return false;
+  if (residual && !device_buffer(h, residual, 16)) return false;
+  const ByteRange w(h->w, n * row), m(h->m, n * (size_t)h->stride * m_elem_size(h));
+  const ByteRange msg(messages, n * (size_t)packed_bytes(h->cfg.n_params));
+  const ByteRange b = base ? ByteRange(base, (size_t)h->cfg.n_params * elem_size(h)) : ByteRange();
+  const ByteRange e = residual ? ByteRange(residual, n * (size_t)h->stride * sizeof(float)) : ByteRange();
+  if (msg.meets(w) || msg.meets(m)) return false;
+  if (residual && (e.meets(w) || e.meets(m) || e.meets(msg))) return false;
+  if (!base) return true;
+  const bool is_row = b.lo >= w.lo && b.hi <= w.hi && (b.lo - w.lo) % row == 0;
+  return (is_row || !b.meets(w)) && !b.meets(m) && !b.meets(msg) && !(residual && b.meets(e));
+}
+
+#ifdef HADFL_DEBUG
+int keep_exchange_buffers(const hadfl_handle *h, const void *base, const void *residual, const void *messages) {
+  const size_t n = (size_t)h->cfg.n_devices;
+  int bad = debug_keep(messages, n * (size_t)packed_bytes(h->cfg.n_params));
+  if (base) bad |= debug_keep(base, (size_t)h->cfg.n_params * elem_size(h));
+  if (residual) bad |= debug_keep(residual, n * (size_t)h->stride * sizeof(float));
+  return bad;
+}
+#define HADFL_KEEP(...)                                             \
+  do {                                                              \
+    if (keep_exchange_buffers(__VA_ARGS__)) return HADFL_ERR_CUDA; \
+  } while (0)
+#else
+#define HADFL_KEEP(...) \
+  do {                  \
+  } while (0)
+#endif
+
+PackedShape packed_shape(const hadfl_handle *h) {
+  return PackedShape{h->w, h->stride, h->cfg.n_params, h->cfg.dtype == HADFL_DTYPE_BF16, h->sm_count, h->stream};
+}
+
+PackedRows packed_rows(const int32_t *ids, int n) {
+  PackedRows r;
+  r.n = n;
+  for (int j = 0; j < kPackedMaxRows; ++j) r.id[j] = j < n ? ids[j] : 0;
+  return r;
+}
+
+}  // namespace
+
+int hadfl_pack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const void *base, float *residual,
+               int32_t rounding, int64_t round, void *messages) {
+  if (!h || !distinct_ids(h, device_ids, n)) return HADFL_ERR_INVALID;
+  if (rounding != HADFL_ROUND_NEAREST && rounding != HADFL_ROUND_STOCHASTIC) return HADFL_ERR_INVALID;
+  if (round < 0 || round >> 56) return HADFL_ERR_INVALID;
+  DeviceGuard guard(h->device);
+  if (!exchange_buffers(h, base, residual, messages)) return HADFL_ERR_INVALID;
+  HADFL_KEEP(h, base, residual, messages);
+  launch_pack(packed_shape(h), packed_rows(device_ids, n), base, residual, rounding == HADFL_ROUND_STOCHASTIC,
+              (uint64_t)round, h->keys, (uint8_t *)messages);
+  return check_launch(h);
+}
+
+int hadfl_unpack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const void *base, const void *messages) {
+  if (!h || !distinct_ids(h, device_ids, n)) return HADFL_ERR_INVALID;
+  DeviceGuard guard(h->device);
+  if (!exchange_buffers(h, base, nullptr, messages)) return HADFL_ERR_INVALID;
+  HADFL_KEEP(h, base, nullptr, messages);
+  launch_unpack(packed_shape(h), packed_rows(device_ids, n), base, (const uint8_t *)messages);
+  return check_launch(h);
+}
+
+int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, const double *versions, void *base,
+                           int32_t move_base, const int32_t *dst_ids, int32_t n, const void *messages) {
+  if (!h || !distinct_ids(h, selected, k) || (move_base && !base)) return HADFL_ERR_INVALID;
+  if (!dst_ids && n == 0) {
+    dst_ids = selected;
+    n = k;
+  }
+  if (!distinct_ids(h, dst_ids, n)) return HADFL_ERR_INVALID;
+  DeviceGuard guard(h->device);
+  if (!exchange_buffers(h, base, nullptr, messages)) return HADFL_ERR_INVALID;
+  HADFL_KEEP(h, base, nullptr, messages);
+  PackedWeights from;
+  memset(&from, 0, sizeof(from));
+  from.k = k;
+  double x[kMaxDevices];
+  scaled_versions(h, versions, x);
+  aggregation_weights(h->cfg.weight_mode, x, h->avail, h->cfg.n_devices, selected, k, from.a);
+  for (int j = 0; j < k; ++j) from.id[j] = selected[j];
+  launch_aggregate_packed(packed_shape(h), from, packed_rows(dst_ids, n), base, move_base != 0,
+                          (const uint8_t *)messages);
+  const int rc = check_launch(h);
+  if (rc != HADFL_OK) return rc;
+  uint32_t vmax = 0;
+  for (int j = 0; j < k; ++j) vmax = h->version[selected[j]] > vmax ? h->version[selected[j]] : vmax;
+  for (int j = 0; j < n; ++j) h->version[dst_ids[j]] = vmax;
+  return HADFL_OK;
+}
+
+int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const void *a_messages, const int32_t *b_ids,
+                      int32_t n, const void *b_messages, float *out) {
+  if (!h) return HADFL_ERR_INVALID;
+  if (!b_ids && !b_messages && n == 0) {
+    b_ids = a_ids;
+    b_messages = a_messages;
+    n = m;
+  }
+  const int N = h->cfg.n_devices;
+  if (!a_ids || !b_ids || m < 1 || m > N || n < 1 || n > N) return HADFL_ERR_INVALID;
+  for (int j = 0; j < m; ++j)
+    if (a_ids[j] < 0 || a_ids[j] >= N) return HADFL_ERR_INVALID;
+  for (int j = 0; j < n; ++j)
+    if (b_ids[j] < 0 || b_ids[j] >= N) return HADFL_ERR_INVALID;
+  DeviceGuard guard(h->device);
+  const size_t bytes = (size_t)N * (size_t)packed_bytes(h->cfg.n_params), out_bytes = sizeof(float) * (size_t)(m * n);
+  if (!device_buffer(h, a_messages, 16) || !device_buffer(h, b_messages, 16) || !device_buffer(h, out, 4))
+    return HADFL_ERR_INVALID;
+  const ByteRange o(out, out_bytes);
+  if (o.meets(ByteRange(a_messages, bytes)) || o.meets(ByteRange(b_messages, bytes))) return HADFL_ERR_INVALID;
+  if (o.meets(ByteRange(h->w, (size_t)N * (size_t)h->stride * elem_size(h))) ||
+      o.meets(ByteRange(h->m, (size_t)N * (size_t)h->stride * m_elem_size(h))))
+    return HADFL_ERR_INVALID;
+  HADFL_KEEP(h, nullptr, nullptr, a_messages);
+  HADFL_KEEP(h, nullptr, nullptr, b_messages);
+#ifdef HADFL_DEBUG
+  if (debug_keep(out, out_bytes)) return HADFL_ERR_CUDA;
+#endif
+  launch_packed_dots(packed_shape(h), packed_rows(a_ids, m), (const uint8_t *)a_messages, packed_rows(b_ids, n),
+                     (const uint8_t *)b_messages, out, h->d_dots);
+  return check_launch(h);
 }
 
 int hadfl_set_sync_beta(hadfl_handle *h, float beta) {
