@@ -1248,8 +1248,8 @@ int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const vo
 #ifdef HADFL_DEBUG
   if (debug_keep(out, out_bytes)) return HADFL_ERR_CUDA;
 #endif
-  launch_packed_dots(packed_shape(h), packed_rows(a_ids, m), (const uint8_t *)a_messages, packed_rows(b_ids, n),
-                     (const uint8_t *)b_messages, out, h->d_dots);
+  HADFL_CUDA(h, launch_packed_dots(packed_shape(h), packed_rows(a_ids, m), (const uint8_t *)a_messages,
+                                   packed_rows(b_ids, n), (const uint8_t *)b_messages, out, h->d_dots));
   return check_launch(h);
 }
 

@@ -642,12 +642,6 @@ k_integrate(WT *__restrict__ w, int64_t stride, int64_t n_params, MixArgs a) {
 // ------------------------------------------------------------------------------------------
 // Deterministic reductions shared by the statistics kernel and the fused round kernel.
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
-  return v;
-}
-
 // The finish's sums: emit(t, sum of src[t][0 .. n_src)) for every t < n_vals, by one block, in a fixed order
 // (a warp per value, lanes strided, then the butterfly).  Often only this block is still running, so
 // what counts is latency: a warp takes 2 values at a time and has up to 8 loads in flight.  Measured

@@ -2,6 +2,7 @@
 #include "packed.cuh"
 
 #include <stddef.h>
+#include <string.h>
 
 #include <type_traits>
 
@@ -100,24 +101,37 @@ void launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights,
 }
 
 size_t packed_dots_scratch_bytes(int sm_count) {
-  return sizeof(double) * (size_t)sm_count * 4 * kPackedMaxRows * kPackedMaxRows;
+  return sizeof(double) * (size_t)sm_count * kPackedMaxRows * kPackedMaxRows;
 }
 
-void launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
-                        const uint8_t *b, float *out, void *scratch) {
+cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
+                               const uint8_t *b, float *out, void *scratch) {
   DotsParams q;
   q.a = a_rows;
   q.b = b_rows;
-  q.n_params = s.n_params;
+  q.same = a == b && a_rows.n == b_rows.n && memcmp(a_rows.id, b_rows.id, sizeof(a_rows.id)) == 0;
+  const int most = a_rows.n > b_rows.n ? a_rows.n : b_rows.n;
+  q.rows = 1;
+  while (q.rows < most) q.rows *= 2;
+  q.segments = kDotsThreads / q.rows;
+  q.blocks = (s.n_params + kPackedBlock - 1) / kPackedBlock;
   q.scales_at = packed_scales_at(s.n_params);
   q.message_bytes = packed_bytes(s.n_params);
-  const int64_t tiles = (s.n_params + kDotsColumns - 1) / kDotsColumns;
-  const int64_t most = (int64_t)s.sm_count * 4;
-  const int blocks = (int)(tiles < most ? tiles : most);
-  k_packed_dots<<<blocks, kThreads, 0, s.stream>>>(a, b, (double *)scratch, q);
+  const int64_t pieces = (s.n_params + kDotsPiece - 1) / kDotsPiece;
+  q.tiles = (pieces + q.segments - 1) / q.segments;
+  const int blocks = (int)(q.tiles < s.sm_count ? q.tiles : s.sm_count);
   const int pairs = a_rows.n * b_rows.n;
-  k_packed_dots_finish<<<(pairs + kThreads - 1) / kThreads, kThreads, 0, s.stream>>>((const double *)scratch, blocks, pairs,
-                                                                                    out);
+  cudaError_t rc = cudaSuccess;
+  with_flag(q.same != 0, [&](auto same) {
+    auto kernel = k_packed_dots<same.value>;
+    const int bytes = 1024 + (same.value ? kDotsMaxStages * kDotsSetBytes : 4 * 2 * kDotsSetBytes);
+    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (rc == cudaSuccess) kernel<<<blocks, kDotsThreads, bytes, s.stream>>>(a, b, (double *)scratch, q);
+  });
+  if (rc != cudaSuccess) return rc;
+  k_packed_dots_finish<<<(pairs + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, s.stream>>>(
+      (const double *)scratch, blocks, a_rows.n, b_rows.n, q.same, out);
+  return cudaSuccess;
 }
 
 #ifdef HADFL_DEBUG

@@ -52,8 +52,8 @@ void launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights,
 // out[i * b_rows.n + j] = sum over the parameters of message a_rows.id[i] of a times message b_rows.id[j] of b.
 // scratch: packed_dots_scratch_bytes() bytes.
 size_t packed_dots_scratch_bytes(int sm_count);
-void launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
-                        const uint8_t *b, float *out, void *scratch);
+cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
+                               const uint8_t *b, float *out, void *scratch);
 
 // Debug build: this file's kernels have a range table of their own.
 int packed_debug_publish(const void *table, size_t bytes);

@@ -270,6 +270,12 @@ __device__ __forceinline__ int live_of(std::false_type, int64_t n_params, int64_
   return live_of(n_params, p, E);
 }
 
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
+  return v;
+}
+
 // Whether this block draws the last of n tickets; what it wrote before is visible to the block that does.
 __device__ __forceinline__ bool is_last_block(unsigned int *__restrict__ ticket, unsigned int n, bool *s_last) {
   __threadfence();
