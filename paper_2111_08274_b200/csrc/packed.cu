@@ -31,8 +31,33 @@ void with_storage(bool bf16, F &&f) {
     f(Type<float>{});
 }
 
-unsigned column_blocks(int64_t columns) {
-  return (unsigned)((columns + (int64_t)kThreads * kPackedE - 1) / ((int64_t)kThreads * kPackedE));
+// Blocks of kThreads threads that cover the columns.
+unsigned column_blocks(bool bf16, int64_t columns) {
+  const int64_t per_block = (int64_t)kThreads * (bf16 ? PackedE<__nv_bfloat16>::value : PackedE<float>::value);
+  return (unsigned)((columns + per_block - 1) / per_block);
+}
+
+bool at_32(const void *p) { return ((uintptr_t)p & 31u) == 0; }
+
+// The rows of a pack or unpack launch, and how many of them a block walks over: all, so that the base is loaded once, but
+// fewer where the columns alone make less than two blocks per SM.  Measured, us, all rows / split: pack, 2 of 100,000 fp32
+// parameters (25 or 49 blocks of columns) 2.40 / 1.96; 32 of 200,000 fp32 (98 blocks) 11.8 / 6.6; 16 of 300,000 bf16 (74)
+// 6.3 / 5.7; from two blocks per SM on no split: 16 of 1 M fp32 (489) 33.1 / 37.1.
+template <typename Params>
+unsigned split_rows(const PackedShape &s, const PackedRows &rows, int64_t columns, Params &q) {
+  const unsigned blocks = column_blocks(s.bf16, columns);
+  const unsigned sms = (unsigned)s.sm_count;
+  const int split = blocks < 2 * sms ? (int)((4 * sms + blocks - 1) / blocks) : 1;
+  q.n = rows.n;
+  q.rows_per_block = split < rows.n ? (rows.n + split - 1) / split : 1;
+  q.row_blocks = (rows.n + q.rows_per_block - 1) / q.rows_per_block;
+  q.n_params = s.n_params;
+  q.scales_at = packed_scales_at(s.n_params);
+  for (int j = 0; j < rows.n; ++j) {
+    q.row_at[j] = rows.id[j] * s.stride;
+    q.message_at[j] = rows.id[j] * packed_bytes(s.n_params);
+  }
+  return blocks * (unsigned)q.row_blocks;
 }
 
 }  // namespace
@@ -40,24 +65,27 @@ unsigned column_blocks(int64_t columns) {
 void launch_pack(const PackedShape &s, const PackedRows &rows, const void *base, float *residual, bool stochastic,
                  uint64_t round, const PhiloxKeys &keys, uint8_t *messages) {
   PackParams q;
-  q.rows = rows;
-  q.rows_per_block = rows.n;
-  q.round_lo = (uint32_t)round;
+  const int64_t scales_at = packed_scales_at(s.n_params);
+  q.code_columns = scales_at * 2;
+  q.scale_columns = (packed_bytes(s.n_params) - scales_at) * kPackedBlock;
+  const unsigned grid = split_rows(s, rows, q.scale_columns, q);
   q.tag = kTagPack | ((uint32_t)(round >> 32) & 0xFFFFFFu);
-  q.n_params = s.n_params;
-  q.stride = s.stride;
-  q.scales_at = packed_scales_at(s.n_params);
-  q.message_bytes = packed_bytes(s.n_params);
-  q.code_columns = q.scales_at * 2;
-  q.scale_columns = (q.message_bytes - q.scales_at) * kPackedBlock;
-  const dim3 grid(column_blocks(q.scale_columns), (unsigned)((rows.n + q.rows_per_block - 1) / q.rows_per_block));
+  for (int j = 0; j < rows.n; ++j) {
+    // The rounds of the generator that the device takes part in alone (see random_words).
+    const uint64_t p1 = (uint64_t)kPhiloxM1 * (uint32_t)rows.id[j];
+    const uint64_t p0 = (uint64_t)kPhiloxM0 * ((uint32_t)(p1 >> 32) ^ (uint32_t)round ^ keys.a[0]);
+    q.random[j] = RowRandom{(uint32_t)p1 ^ keys.a[1], (uint32_t)(p0 >> 32) ^ keys.b[1], (uint32_t)p0};
+  }
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;
     with_flag(base != nullptr, [&](auto has_base) {
       with_flag(residual != nullptr, [&](auto has_residual) {
         with_flag(stochastic, [&](auto is_stochastic) {
-          k_pack<WT, has_base.value, has_residual.value, is_stochastic.value><<<grid, kThreads, 0, s.stream>>>(
-              (const WT *)s.w, (const WT *)base, residual, messages, keys, q);
+          with_flag(at_32(residual), [&](auto is_at_32) {
+            if constexpr (has_residual.value || is_at_32.value)  // without a residual there are no stores to rows
+              k_pack<WT, has_base.value, has_residual.value, is_stochastic.value, is_at_32.value>
+                  <<<grid, kThreads, 0, s.stream>>>((const WT *)s.w, (const WT *)base, residual, messages, keys, q);
+          });
         });
       });
     });
@@ -66,17 +94,14 @@ void launch_pack(const PackedShape &s, const PackedRows &rows, const void *base,
 
 void launch_unpack(const PackedShape &s, const PackedRows &rows, const void *base, const uint8_t *messages) {
   UnpackParams q;
-  q.rows = rows;
-  q.rows_per_block = rows.n;
-  q.n_params = s.n_params;
-  q.stride = s.stride;
-  q.scales_at = packed_scales_at(s.n_params);
-  q.message_bytes = packed_bytes(s.n_params);
-  const dim3 grid(column_blocks(s.n_params), (unsigned)((rows.n + q.rows_per_block - 1) / q.rows_per_block));
+  const unsigned grid = split_rows(s, rows, s.n_params, q);
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;
     with_flag(base != nullptr, [&](auto has_base) {
-      k_unpack<WT, has_base.value><<<grid, kThreads, 0, s.stream>>>((WT *)s.w, (const WT *)base, messages, q);
+      with_flag(at_32(s.w) && s.stride % (int64_t)(32 / sizeof(WT)) == 0, [&](auto is_at_32) {
+        k_unpack<WT, has_base.value, is_at_32.value><<<grid, kThreads, 0, s.stream>>>((WT *)s.w, (const WT *)base, messages,
+                                                                                     q);
+      });
     });
   });
 }
@@ -84,18 +109,24 @@ void launch_unpack(const PackedShape &s, const PackedRows &rows, const void *bas
 void launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights, const PackedRows &receivers, void *base,
                              bool move_base, const uint8_t *messages) {
   AggregateParams q;
-  q.from = weights;
-  q.to = receivers;
+  q.k = weights.k;
+  q.n = receivers.n;
   q.move_base = move_base;
   q.n_params = s.n_params;
-  q.stride = s.stride;
   q.scales_at = packed_scales_at(s.n_params);
-  q.message_bytes = packed_bytes(s.n_params);
+  for (int j = 0; j < q.k; ++j) {
+    q.a[j] = weights.a[j];
+    q.message_at[j] = weights.id[j] * packed_bytes(s.n_params);
+  }
+  for (int j = 0; j < q.n; ++j) q.row_at[j] = receivers.id[j] * s.stride;
+  const unsigned grid = column_blocks(s.bf16, s.n_params);
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;
     with_flag(base != nullptr, [&](auto has_base) {
-      k_aggregate_packed<WT, has_base.value><<<column_blocks(s.n_params), kThreads, 0, s.stream>>>((WT *)s.w, (WT *)base,
-                                                                                                  messages, q);
+      with_flag(at_32(s.w) && at_32(base) && s.stride % (int64_t)(32 / sizeof(WT)) == 0, [&](auto is_at_32) {
+        k_aggregate_packed<WT, has_base.value, is_at_32.value><<<grid, kThreads, 0, s.stream>>>((WT *)s.w, (WT *)base,
+                                                                                               messages, q);
+      });
     });
   });
 }
@@ -109,11 +140,11 @@ cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, c
   DotsParams q;
   q.a = a_rows;
   q.b = b_rows;
-  q.same = a == b && a_rows.n == b_rows.n && memcmp(a_rows.id, b_rows.id, sizeof(a_rows.id)) == 0;
+  const bool same = a == b && a_rows.n == b_rows.n && memcmp(a_rows.id, b_rows.id, sizeof(a_rows.id)) == 0;
   const int most = a_rows.n > b_rows.n ? a_rows.n : b_rows.n;
   q.rows = 1;
   while (q.rows < most) q.rows *= 2;
-  q.segments = kDotsThreads / q.rows;
+  q.segments = kDotsRows / q.rows;
   q.blocks = (s.n_params + kPackedBlock - 1) / kPackedBlock;
   q.scales_at = packed_scales_at(s.n_params);
   q.message_bytes = packed_bytes(s.n_params);
@@ -121,17 +152,27 @@ cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, c
   q.tiles = (pieces + q.segments - 1) / q.segments;
   const int blocks = (int)(q.tiles < s.sm_count ? q.tiles : s.sm_count);
   const int pairs = a_rows.n * b_rows.n;
+  double *partials = (double *)scratch;
   cudaError_t rc = cudaSuccess;
-  with_flag(q.same != 0, [&](auto same) {
-    auto kernel = k_packed_dots<same.value>;
-    const int bytes = 1024 + (same.value ? kDotsMaxStages * kDotsSetBytes : 4 * 2 * kDotsSetBytes);
+  with_flag(same, [&](auto is_same) {
+    using Stages = DotsStages<is_same.value>;
+    auto kernel = k_packed_dots<is_same.value>;
+    const int bytes = 1024 + Stages::value * Stages::bytes;
     rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (rc == cudaSuccess) kernel<<<blocks, kDotsThreads, bytes, s.stream>>>(a, b, (double *)scratch, q);
+    if (rc == cudaSuccess) kernel<<<blocks, kDotsThreads, bytes, s.stream>>>(a, b, partials, q);
   });
   if (rc != cudaSuccess) return rc;
-  k_packed_dots_finish<<<(pairs + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, s.stream>>>(
-      (const double *)scratch, blocks, a_rows.n, b_rows.n, q.same, out);
-  return cudaSuccess;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3((unsigned)((pairs + kThreads / 32 - 1) / (kThreads / 32)));
+  config.blockDim = dim3(kThreads);
+  config.stream = s.stream;
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, k_packed_dots_finish, (const double *)partials, blocks, (int)a_rows.n, (int)b_rows.n,
+                            (int)same, out);
 }
 
 #ifdef HADFL_DEBUG

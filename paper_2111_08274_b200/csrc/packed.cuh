@@ -6,8 +6,8 @@
 // 2^-127 or larger, with A <= 6 * scale: no value is cut off, so stochastic rounding is free of bias and the residual of
 // a block at most one scale.
 //
-// All of it streams: 8 consecutive parameters per thread, four threads per block of 32, so that a warp's loads are 1 KB
-// of fp32 parameters, its codes one line of 128 bytes, its scales 8 bytes.
+// All of it streams: a thread has 32 bytes of a row of parameters, 8 fp32 or 16 bf16 values, and four or two
+// threads a block of 32, so that a warp's codes are one or two lines of 128 bytes.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_fp4.h>
@@ -17,8 +17,74 @@
 
 namespace hadfl {
 
-constexpr int kPackedE = 8;  // parameters per thread
 constexpr uint32_t kPackedNan = 255;
+
+// Parameters per thread, in parts of 8.
+template <typename WT>
+struct PackedE {
+  static constexpr int value = 32 / (int)sizeof(WT), parts = value / 8;
+};
+
+// E consecutive values of a row as they come from memory.
+template <typename T, int kParts>
+struct RawParts {
+  RawPack<T, 8> part[kParts];
+};
+// live: how many of the values there are; FullPack<8 * kParts> where all are.
+template <typename T, int kParts, typename Live>
+__device__ __forceinline__ void ld_parts(const T *at, Live live, RawParts<T, kParts> &r) {
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    if constexpr (std::is_same_v<Live, int>) {
+      const int here = min(max(live - 8 * i, 0), 8);
+      zero_raw(r.part[i]);
+      if (here > 0) ld_raw(at + 8 * i, here, r.part[i]);
+    } else {
+      ld_raw(at + 8 * i, 8, r.part[i]);
+    }
+  }
+}
+struct Eight {
+  __device__ constexpr operator int() const { return 8; }
+};
+// Values to a row, rounded to its storage type.  k32: the row starts at a multiple of 32 bytes; whole 32 bytes then go out
+// in one store (two of 16 write half of each 32-byte sector at a time, see st_full).
+template <bool k32, typename T, int E, typename Live>
+__device__ __forceinline__ void st_parts(T *at, Live live, const float (&v)[E]) {
+  if constexpr (k32 && sizeof(T) == 2) {
+    if (live >= E) {
+      if (!access_ok(at, 2 * E)) return;
+      uint32_t x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = floats_to_bf16x2(v[2 * i], v[2 * i + 1]);
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]),
+                   "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+                   : "memory");
+      return;
+    }
+  }
+  if constexpr (std::is_same_v<Live, int> || !k32 || sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < E / 8; ++i) {
+      const int here = min(live - 8 * i, 8);
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = v[8 * i + j];
+      if (here == 8)
+        st_pack_any(at + 8 * i, 0, std::conditional_t<k32, FullPack<8>, Eight>{}, x);
+      else if (here > 0)
+        st_pack_any(at + 8 * i, 0, here, x);
+    }
+  }
+}
+// Calls f(live) for a thread's columns, with FullPack where all columns of the block are there.
+template <int E, typename F>
+__device__ __forceinline__ void with_live(int64_t n_params, int64_t block, F &&f) {
+  if (E * kThreads * (block + 1) <= n_params)
+    f(FullPack<E>{});
+  else
+    f(live_of(n_params, block * kThreads + threadIdx.x, E));
+}
 
 // 2^(byte - 127), NaN for 255.
 __device__ __forceinline__ float packed_scale(uint32_t byte) {
@@ -27,7 +93,7 @@ __device__ __forceinline__ float packed_scale(uint32_t byte) {
 }
 
 // The values of 8 codes, without their scale.
-__device__ __forceinline__ void packed_values(uint32_t codes, float (&v)[kPackedE]) {
+__device__ __forceinline__ void packed_values(uint32_t codes, float *v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(codes >> (8 * i)), __NV_E2M1);
@@ -37,7 +103,8 @@ __device__ __forceinline__ void packed_values(uint32_t codes, float (&v)[kPacked
   }
 }
 
-__device__ __forceinline__ uint32_t packed_codes(const float (&y)[kPackedE]) {
+// 8 values y (|y| <= 6) as codes, rounded to nearest, ties to even.
+__device__ __forceinline__ uint32_t packed_codes(const float *y) {
   uint32_t codes = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -46,198 +113,318 @@ __device__ __forceinline__ uint32_t packed_codes(const float (&y)[kPackedE]) {
   return codes;
 }
 
-// |y| <= 6 to a neighbour on the e2m1 grid, away from zero with probability (way from the lower one) / (spacing): 16
-// random bits are added to the upper 16 of the 22 mantissa bits that e2m1 does not have, and the 22 bits dropped.  Below
-// 1 the grid is evenly spaced, as it is from 1 to 2, where the sum with 1 is.
-__device__ __forceinline__ float packed_stochastic(float y, uint32_t r16) {
-  const float t = fabsf(y);
-  const bool small = t < 1.0f;
-  float z = small ? __fadd_rn(t, 1.0f) : t;
-  z = __uint_as_float((__float_as_uint(z) + (r16 << 6)) & 0xFFC00000u);
-  return copysignf(small ? z - 1.0f : z, y);
+// ... rounded away from zero with probability (way from the lower value) / (distance of the two).  t = y * 2^-126 has |y| = 1
+// at the smallest normal number, so that its bits have the spacing of e2m1 throughout - even below 1, where both formats
+// are subnormal - and bits 22 to 24 are the code.  (t is rounded to 2^-23 of y's unit, as fl(|y| + 1) is.)  The 16
+// random bits are added to the upper 16 of the 22 bits below, a carry is the step up.  Codes and signs are then gathered
+// in 16-bit halves, parameters i and i + 4 in one word, so that a shift or a mask is for two of them.
+__device__ __forceinline__ uint32_t packed_codes_stochastic(const float *t, const uint32_t (&r)[4]) {
+  uint32_t up[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) up[i] = __float_as_uint(t[i]) + ((i & 1 ? r[i / 2] >> 16 : r[i / 2] & 0xFFFFu) << 6);
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t two = __byte_perm(up[i], up[i + 4], 0x7632);  // in each half: the sign at 15, the code at 6 to 8
+    const uint32_t magnitude = 4 * i < 6 ? two >> (6 - 4 * i) : two << (4 * i - 6);
+    codes |= (magnitude & 0x00070007u << 4 * i) | (two >> (12 - 4 * i) & 0x00080008u << 4 * i);
+  }
+  return codes;
+}
+
+// Random words of the 8 parameters of a group: the first two rounds of Philox4x32-10 on the counter (group, round, device,
+// tag), split into what depends on the group alone (once per thread), on the device alone (on the host: RowRandom) and
+// the three exclusive ors of both.
+struct RowRandom {
+  uint32_t c0, c2, c3;
+};
+struct GroupRandom {
+  uint32_t a, b, c;
+};
+__device__ __forceinline__ GroupRandom group_random(uint32_t group, uint32_t tag, const PhiloxKeys &k) {
+  const unsigned long long p0 = (unsigned long long)kPhiloxM0 * group;
+  const unsigned long long p1 = (unsigned long long)kPhiloxM1 * ((uint32_t)(p0 >> 32) ^ tag ^ k.b[0]);
+  return GroupRandom{(uint32_t)(p1 >> 32), (uint32_t)p1, (uint32_t)p0};
+}
+__device__ __forceinline__ void random_words(const GroupRandom &g, const RowRandom &row, const PhiloxKeys &k,
+                                             uint32_t (&r)[4]) {
+  r[0] = g.a ^ row.c0;
+  r[1] = g.b;
+  r[2] = g.c ^ row.c2;
+  r[3] = row.c3;
+#pragma unroll
+  for (int i = 2; i < 10; ++i) philox_round(r[0], r[1], r[2], r[3], k.a[i], k.b[i]);
+}
+
+// The largest magnitude; NaN if there is one.
+__device__ __forceinline__ float max_magnitude(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 struct PackParams {
-  PackedRows rows;
-  int rows_per_block;
-  uint32_t round_lo, tag;  // words 1 and 3 of the rounding's counter
-  int64_t n_params, stride;
+  int n, rows_per_block, row_blocks;
+  uint32_t tag;  // word 3 of the rounding's counter
+  int64_t n_params;
   int64_t code_columns, scale_columns;  // columns that the message's codes and scales have room for
-  int64_t scales_at, message_bytes;
+  int64_t scales_at;
+  int64_t row_at[kPackedMaxRows], message_at[kPackedMaxRows];
+  RowRandom random[kPackedMaxRows];
 };
 
-// Quantisation.  A thread walks over the rows of its 8 columns with the base in registers.
-template <typename WT, bool kBase, bool kResidual, bool kStochastic>
+// Quantisation.  A thread walks over the rows of its columns with the base in registers.
+template <typename WT, bool kBase, bool kResidual, bool kStochastic, bool k32>
 __global__ void __launch_bounds__(kThreads)
 k_pack(const WT *__restrict__ w, const WT *base, float *__restrict__ residual, uint8_t *__restrict__ messages,
        PhiloxKeys keys, const __grid_constant__ PackParams q) {
-  constexpr int E = kPackedE;
-  const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t column = E * p;
+  constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, kLanes = kPackedBlock / E;
+  constexpr bool kPrefetch = !kResidual;
+  const int64_t block = blockIdx.x / q.row_blocks;
+  const int64_t group = block * kThreads + threadIdx.x;
+  const int64_t column = E * group;
   if (column >= q.scale_columns) return;  // whole warps: scale_columns is a multiple of 32 * 128
-  const int live = live_of(q.n_params, p, E);
-  RawPack<WT, E> base_raw;
-  zero_raw(base_raw);
-  if (kBase && live > 0) ld_raw(base + column, live, base_raw);
-  const int first = blockIdx.y * q.rows_per_block;
-  const int end = min(first + q.rows_per_block, q.rows.n);
-  for (int j = first; j < end; ++j) {
-    const int dev = q.rows.id[j];
-    const int64_t row = (int64_t)dev * q.stride;
-    RawPack<WT, E> w_raw;
-    RawPack<float, E> e_raw;
-    zero_raw(w_raw);
-    zero_raw(e_raw);
-    if (live > 0) {
-      ld_raw(w + row + column, live, w_raw);
-      if (kResidual) ld_raw(residual + row + column, live, e_raw);
-    }
-    float u[E];
-    unpack(w_raw, u);
-    if (kBase) {
-      float b[E];
-      unpack(base_raw, b);
-#pragma unroll
-      for (int i = 0; i < E; ++i) u[i] = __fsub_rn(u[i], b[i]);
-    }
-    if (kResidual) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) u[i] = __fadd_rn(u[i], e_raw.v[i]);
-    }
-    // The largest magnitude of the block, as bits: infinities and NaNs are above all finite values.
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) most = max(most, __float_as_uint(u[i]) & 0x7FFFFFFFu);
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-    const bool lost = most > 0x7F400000u;  // above 6 * 2^125: a larger scale's codes 4 to 6 would read as infinities
-    // A = m 2^E: the scale's exponent is E - 2 for m <= 1.5, else E - 1; the sum carries into the exponent where m > 1.5.
-    const int exponent = (int)((most + 0x3FFFFFu) >> 23) - 2;
-    const uint32_t byte = lost ? kPackedNan : (uint32_t)max(exponent, 0);
-    const float inverse = __uint_as_float((254u - byte) << 23);
-    float y[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = __fmul_rn(u[i], inverse);
+  const int first = blockIdx.x % q.row_blocks * q.rows_per_block;
+  const int end = min(first + q.rows_per_block, q.n);
+  with_live<E>(q.n_params, block, [&](auto live) {
+    RawParts<WT, kParts> base_raw;
+    if (kBase) ld_parts(base + column, live, base_raw);
+    GroupRandom group_part[kParts];
     if (kStochastic) {
-      uint32_t c0 = (uint32_t)p, c1 = q.round_lo, c2 = (uint32_t)dev, c3 = q.tag;
-      philox4x32_10(c0, c1, c2, c3, keys);
-      const uint32_t r[4] = {c0, c1, c2, c3};
 #pragma unroll
-      for (int i = 0; i < E; ++i) y[i] = packed_stochastic(y[i], i & 1 ? r[i / 2] >> 16 : r[i / 2] & 0xFFFFu);
+      for (int i = 0; i < kParts; ++i) group_part[i] = group_random((uint32_t)(group * kParts + i), q.tag, keys);
     }
-    const uint32_t codes = lost ? 0u : packed_codes(y);
-    uint8_t *message = messages + (int64_t)dev * q.message_bytes;
-    if (column < q.code_columns && access_ok(message + column / 2, 4)) *reinterpret_cast<uint32_t *>(message + column / 2) = codes;
-    if ((threadIdx.x & 3) == 0) {
-      uint8_t *at = message + q.scales_at + column / kPackedBlock;
-      if (access_ok(at, 1)) *at = (uint8_t)byte;
-    }
-    if (kResidual && live > 0) {
-      float v[E];
-      packed_values(codes, v);
-      const float scale = packed_scale(byte);
+    struct Row {
+      RawParts<WT, kParts> w;
+      RawParts<float, kParts> e;
+    };
+    auto load = [&](int j, Row &r) {
+      const int64_t at = q.row_at[j] + column;
+      ld_parts(w + at, live, r.w);
+      if (kResidual) ld_parts(residual + at, live, r.e);
+    };
+    Row next;
+    if (kPrefetch) load(first, next);
+#pragma unroll(kPrefetch ? 2 : 1)
+    for (int j = first; j < end; ++j) {
+      Row row;
+      if (kPrefetch) {
+        row = next;
+        if (j + 1 < end) load(j + 1, next);
+      } else {
+        load(j, row);
+      }
+      float u[E];
 #pragma unroll
-      for (int i = 0; i < E; ++i) v[i] = lost ? 0.f : __fsub_rn(u[i], v[i] * scale);
-      st_pack_any(residual + row, p, live, v);
+      for (int i = 0; i < kParts; ++i) {
+        float v[8];
+        unpack(row.w.part[i], v);
+        if (kBase) {
+          float b[8];
+          unpack(base_raw.part[i], b);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = __fsub_rn(v[k], b[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[8 * i + k] = kResidual ? __fadd_rn(v[k], row.e.part[i].v[k]) : v[k];
+      }
+      // The largest magnitude of the block, as bits: infinities and NaNs are above all finite values.
+      float most_here = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; i += 2) most_here = max_magnitude(most_here, u[i], u[i + 1]);
+      uint32_t most = __float_as_uint(most_here);
+#pragma unroll
+      for (int lanes = 1; lanes < kLanes; lanes *= 2) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, lanes));
+      const bool lost = most > 0x7F400000u;  // above 6 * 2^125: a larger scale's codes 4 to 6 would read as infinities
+      // A = m 2^E: the scale's exponent is E - 2 for m <= 1.5, else E - 1; the sum carries into the exponent where m > 1.5.
+      const int exponent = (int)((most + 0x3FFFFFu) >> 23) - 2;
+      const uint32_t byte = lost ? kPackedNan : (uint32_t)max(exponent, 0);
+      uint32_t codes[kParts];
+      if (kStochastic) {
+        // 2^-(s + 126); where that is no number of fp32 (s > 23), 2^-110 is taken off before.  (What then underflows is below
+        // 2^-40 of the scale: 0 in t either way.)
+        const bool large = byte > 127u + 23u;
+        const float down = large ? 0x1p-110f : 1.0f;
+        const uint32_t biased = 128u + (large ? 110u : 0u) - byte;  // exponent + 127 of what is left
+        const float to_t = (int)biased > 0 ? __uint_as_float(biased << 23) : __uint_as_float(0x00400000u >> -(int)biased);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+          float t[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] = u[8 * i + k];
+          if (large) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = __fmul_rn(t[k], down);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] = __fmul_rn(t[k], to_t);
+          uint32_t r[4];
+          random_words(group_part[i], q.random[j], keys, r);
+          codes[i] = packed_codes_stochastic(t, r);
+        }
+      } else {
+        const float inverse = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = __fmul_rn(u[8 * i + k], inverse);
+          codes[i] = packed_codes(y);
+        }
+      }
+      if (lost) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) codes[i] = 0;
+      }
+      uint8_t *message = messages + q.message_at[j];
+      if (column < q.code_columns && access_ok(message + column / 2, 4 * kParts)) {
+        if constexpr (kParts == 2)
+          *reinterpret_cast<uint2 *>(message + column / 2) = make_uint2(codes[0], codes[1]);
+        else
+          *reinterpret_cast<uint32_t *>(message + column / 2) = codes[0];
+      }
+      if ((threadIdx.x & (kLanes - 1)) == 0) {
+        uint8_t *at = message + q.scales_at + column / kPackedBlock;
+        if (access_ok(at, 1)) *at = (uint8_t)byte;
+      }
+      if (kResidual && live > 0) {
+        const float scale = packed_scale(byte);
+        float v[E];
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) packed_values(codes[i], v + 8 * i);
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = lost ? 0.f : fmaf(-v[i], scale, u[i]);  // the product is exact
+        st_parts<k32>(residual + q.row_at[j] + column, live, v);
+      }
     }
-  }
+  });
 }
 
-// The 8 codes and the scale byte of a message at a thread's columns (past the last block: zeros).
+// The codes and the scale byte of a message at a thread's columns.
+template <int kParts>
 struct RawCodes {
-  uint32_t codes, byte;
+  uint32_t codes[kParts], byte;
 };
-__device__ __forceinline__ RawCodes ld_codes(const uint8_t *message, int64_t column, int64_t scales_at) {
-  RawCodes r{0u, 0u};
-  if (access_ok(message + column / 2, 4)) r.codes = *reinterpret_cast<const uint32_t *>(message + column / 2);
+template <int kParts>
+__device__ __forceinline__ RawCodes<kParts> ld_codes(const uint8_t *message, int64_t column, int64_t scales_at) {
+  RawCodes<kParts> r;
+  memset(&r, 0, sizeof(r));
+  if (access_ok(message + column / 2, 4 * kParts)) {
+    if constexpr (kParts == 2) {
+      const uint2 c = *reinterpret_cast<const uint2 *>(message + column / 2);
+      r.codes[0] = c.x;
+      r.codes[1] = c.y;
+    } else {
+      r.codes[0] = *reinterpret_cast<const uint32_t *>(message + column / 2);
+    }
+  }
   const uint8_t *at = message + scales_at + column / kPackedBlock;
   if (access_ok(at, 1)) r.byte = *at;
   return r;
 }
-__device__ __forceinline__ void packed_decode(const RawCodes &r, float (&d)[kPackedE]) {
-  packed_values(r.codes, d);
+template <int kParts>
+__device__ __forceinline__ void packed_decode(const RawCodes<kParts> &r, float (&d)[8 * kParts]) {
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) packed_values(r.codes[i], d + 8 * i);
   const float scale = packed_scale(r.byte);
 #pragma unroll
-  for (int i = 0; i < kPackedE; ++i) d[i] = __fmul_rn(d[i], scale);
+  for (int i = 0; i < 8 * kParts; ++i) d[i] = __fmul_rn(d[i], scale);
 }
 
+// Messages whose loads are in flight together.  Measured, us, 4 / 8: 16 of 32 bf16 devices of 23.5 M parameters 168 / 190,
+// 4 of 8 fp32 devices of 11.2 M 43.0 / 47.0, 32 fp32 devices of 4.2 M 112 / 111.
+constexpr int kPackedBatch = 4;
+
 struct UnpackParams {
-  PackedRows rows;
-  int rows_per_block;
-  int64_t n_params, stride, scales_at, message_bytes;
+  int n, rows_per_block, row_blocks;
+  int64_t n_params, scales_at;
+  int64_t row_at[kPackedMaxRows], message_at[kPackedMaxRows];
 };
 
 // w[i] = base + d_i for the listed devices.
-template <typename WT, bool kBase>
+template <typename WT, bool kBase, bool k32>
 __global__ void __launch_bounds__(kThreads)
 k_unpack(WT *w, const WT *base, const uint8_t *__restrict__ messages, const __grid_constant__ UnpackParams q) {
-  constexpr int E = kPackedE;
-  const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t column = E * p;
-  const int live = live_of(q.n_params, p, E);
-  if (live == 0) return;
-  float b[E];
-  if (kBase) {
-    RawPack<WT, E> raw;
-    ld_raw(base + column, live, raw);
-    unpack(raw, b);
-  }
-  const int first = blockIdx.y * q.rows_per_block;
-  const int end = min(first + q.rows_per_block, q.rows.n);
-  for (int j = first; j < end; ++j) {
-    const int dev = q.rows.id[j];
-    float d[E];
-    packed_decode(ld_codes(messages + (int64_t)dev * q.message_bytes, column, q.scales_at), d);
-    if (kBase) {
+  constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, B = kPackedBatch;
+  const int64_t block = blockIdx.x / q.row_blocks;
+  const int64_t column = E * (block * kThreads + threadIdx.x);
+  const int first = blockIdx.x % q.row_blocks * q.rows_per_block;
+  const int end = min(first + q.rows_per_block, q.n);
+  if (column >= q.n_params) return;
+  with_live<E>(q.n_params, block, [&](auto live) {
+    RawParts<WT, kParts> base_raw;
+    if (kBase) ld_parts(base + column, live, base_raw);
+    for (int j0 = first; j0 < end; j0 += B) {
+      RawCodes<kParts> raw[B];
 #pragma unroll
-      for (int i = 0; i < E; ++i) d[i] = __fadd_rn(b[i], d[i]);
+      for (int j = 0; j < B; ++j)
+        if (j0 + j < end) raw[j] = ld_codes<kParts>(messages + q.message_at[j0 + j], column, q.scales_at);
+#pragma unroll
+      for (int j = 0; j < B; ++j) {
+        if (j0 + j >= end) continue;
+        float d[E];
+        packed_decode(raw[j], d);
+        if (kBase) {
+#pragma unroll
+          for (int i = 0; i < kParts; ++i) {
+            float b[8];
+            unpack(base_raw.part[i], b);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) d[8 * i + k] = __fadd_rn(b[k], d[8 * i + k]);
+          }
+        }
+        st_parts<k32>(w + q.row_at[j0 + j] + column, live, d);
+      }
     }
-    st_pack_any(w + (int64_t)dev * q.stride, p, live, d);
-  }
+  });
 }
 
 struct AggregateParams {
-  PackedWeights from;
-  PackedRows to;
-  int move_base;
-  int64_t n_params, stride, scales_at, message_bytes;
+  int k, n, move_base;
+  int64_t n_params, scales_at;
+  float a[kPackedMaxRows];
+  int64_t row_at[kPackedMaxRows], message_at[kPackedMaxRows];
 };
 
 // Eq. 5 from messages: acc = a_0 d_0, acc = fma(a_j, d_j, acc); base + acc to the receivers and, on request, the base.
-template <typename WT, bool kBase>
+template <typename WT, bool kBase, bool k32>
 __global__ void __launch_bounds__(kThreads)
 k_aggregate_packed(WT *w, WT *base, const uint8_t *__restrict__ messages, const __grid_constant__ AggregateParams q) {
-  constexpr int E = kPackedE, B = 4;
-  const int64_t p = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t column = E * p;
-  const int live = live_of(q.n_params, p, E);
-  if (live == 0) return;
-  RawPack<WT, E> base_raw;
-  if (kBase) ld_raw(base + column, live, base_raw);
-  float acc[E];
-  for (int j0 = 0; j0 < q.from.k; j0 += B) {
-    RawCodes raw[B];
+  constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, B = kPackedBatch;
+  const int64_t block = blockIdx.x;
+  const int64_t column = E * (block * kThreads + threadIdx.x);
+  if (column >= q.n_params) return;
+  with_live<E>(q.n_params, block, [&](auto live) {
+    RawParts<WT, kParts> base_raw;
+    if (kBase) ld_parts((const WT *)base + column, live, base_raw);
+    float acc[E];
+    for (int j0 = 0; j0 < q.k; j0 += B) {
+      RawCodes<kParts> raw[B];
 #pragma unroll
-    for (int j = 0; j < B; ++j)
-      if (j0 + j < q.from.k) raw[j] = ld_codes(messages + (int64_t)q.from.id[j0 + j] * q.message_bytes, column, q.scales_at);
+      for (int j = 0; j < B; ++j)
+        if (j0 + j < q.k) raw[j] = ld_codes<kParts>(messages + q.message_at[j0 + j], column, q.scales_at);
 #pragma unroll
-    for (int j = 0; j < B; ++j) {
-      if (j0 + j >= q.from.k) continue;
-      const float a = q.from.a[j0 + j];
-      float d[E];
-      packed_decode(raw[j], d);
+      for (int j = 0; j < B; ++j) {
+        if (j0 + j >= q.k) continue;
+        const float a = q.a[j0 + j];
+        float d[E];
+        packed_decode(raw[j], d);
 #pragma unroll
-      for (int i = 0; i < E; ++i) acc[i] = j0 + j == 0 ? __fmul_rn(a, d[i]) : fmaf(a, d[i], acc[i]);
+        for (int i = 0; i < E; ++i) acc[i] = j0 + j == 0 ? __fmul_rn(a, d[i]) : fmaf(a, d[i], acc[i]);
+      }
     }
-  }
-  if (kBase) {
-    float b[E];
-    unpack(base_raw, b);
+    if (kBase) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) acc[i] = __fadd_rn(b[i], acc[i]);
-  }
-  for (int j = 0; j < q.to.n; ++j) st_pack_any(w + (int64_t)q.to.id[j] * q.stride, p, live, acc);
-  if (kBase && q.move_base) st_pack_any(base, p, live, acc);
+      for (int i = 0; i < kParts; ++i) {
+        float b[8];
+        unpack(base_raw.part[i], b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[8 * i + k] = __fadd_rn(b[k], acc[8 * i + k]);
+      }
+    }
+    for (int j = 0; j < q.n; ++j) st_parts<k32>(w + q.row_at[j] + column, live, acc);
+    if (kBase && q.move_base) st_parts<k32>(base + column, live, acc);
+  });
 }
 
 // ------------------------------------------------------------------------------------------
@@ -252,14 +439,22 @@ k_aggregate_packed(WT *w, WT *base, const uint8_t *__restrict__ messages, const 
 // The accumulator is fp32 in TMEM, where a long sum of one sign loses bits, so that every kDotsFlush tiles it is added
 // to sums in 64 bits.
 // ------------------------------------------------------------------------------------------
-constexpr int kDotsThreads = 128;   // also the rows of a tile
+// Warps for the copies, for the accumulators' rows, and to ask for the products, each of the latter with an accumulator.
+constexpr int kDotsLoadWarps = 8, kDotsSumWarps = 4, kDotsMmaWarps = 2;
+constexpr int kDotsThreads = 32 * (kDotsLoadWarps + kDotsSumWarps + kDotsMmaWarps);
+constexpr int kDotsRows = 128;      // of a tile
 constexpr int kDotsPiece = 256;     // parameters of a row in a tile: 128 bytes of codes, 8 scales
-constexpr int kDotsMaxStages = 6;
 constexpr int kDotsFlush = 64;      // 2^14 parameters per row
-constexpr int kDotsCodeBytes = kDotsThreads * kDotsPiece / 2;
-constexpr int kDotsScaleBytes = kDotsThreads * kDotsPiece / kPackedBlock;
+constexpr int kDotsCodeBytes = kDotsRows * kDotsPiece / 2;
+constexpr int kDotsScaleBytes = kDotsRows * kDotsPiece / kPackedBlock;
 constexpr int kDotsSetBytes = kDotsCodeBytes + kDotsScaleBytes;
-constexpr int kDotsTmemColumns = 256;  // 128 of the accumulator, 2 x 16 of scales
+constexpr int kDotsTmemColumns = 512;  // the accumulators, 128 each, and the scales of the tiles, up to 80
+// Tiles in shared memory.
+template <bool kSame>
+struct DotsStages {
+  static constexpr int value = kSame ? 8 : 5;
+  static constexpr int bytes = (kSame ? 1 : 2) * kDotsSetBytes;
+};
 constexpr uint32_t kDotsWaitNs = 1000, kDotsMaxWaits = 1u << 20;  // a wait ends after a second or so
 
 struct DotsParams {
@@ -281,20 +476,20 @@ __device__ __forceinline__ void copy_async_16(uint32_t to, const void *from, uin
 __device__ __forceinline__ void copy_async_4(uint32_t to, const void *from, uint32_t bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+// The barrier gets this thread's arrival once its copies so far are there.
+__device__ __forceinline__ void copy_async_arrive(uint64_t *barrier) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(shared_address(barrier)) : "memory");
 }
+__device__ __forceinline__ void copy_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Waits for the barrier's phase, with a limit; false if it ran out.
-__device__ __forceinline__ bool barrier_wait(uint32_t barrier, uint32_t parity) {
+__device__ __forceinline__ bool barrier_wait(uint64_t *barrier, uint32_t parity) {
   for (uint32_t i = 0; i < kDotsMaxWaits; ++i) {
     uint32_t done;
     asm volatile(
         "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
         : "=r"(done)
-        : "r"(barrier), "r"(parity), "r"(kDotsWaitNs)
+        : "r"(shared_address(barrier)), "r"(parity), "r"(kDotsWaitNs)
         : "memory");
     if (done) return true;
   }
@@ -341,64 +536,87 @@ __device__ __forceinline__ void tmem_load_32(uint32_t at, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// One thread's part of a tile's copies: 8 pieces of 16 bytes of codes, and the scales of one row.
+// One thread's part of a tile's copies: four pieces of 16 bytes of codes, and four scales.
 struct DotsLoader {
-  int64_t row[8];         // of the row that piece i belongs to: byte offset of its message, -1 without one
-  int64_t own;            // of row threadIdx.x
-  const uint8_t *messages;
+  static constexpr int kThreadsOf = 32 * kDotsLoadWarps, kPieces = kDotsRows * 8 / kThreadsOf;
+  const uint8_t *codes[kPieces], *scales;  // in tile 0; null where no message fills the row
+  int64_t block[kPieces], scale_block;     // and which block of 32 parameters that is
+  uint32_t to[kPieces], scales_to;         // places in a set
 
-  __device__ __forceinline__ void start(const uint8_t *m, const PackedRows &ids, const DotsParams &q) {
-    messages = m;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) row[i] = offset(ids, q, i * 16 + (threadIdx.x >> 3));
-    own = offset(ids, q, threadIdx.x);
-  }
-  static __device__ __forceinline__ int64_t offset(const PackedRows &ids, const DotsParams &q, int r) {
-    const int i = r & (q.rows - 1);
-    return i < ids.n && r < q.segments * q.rows ? ids.id[i] * q.message_bytes : -1;
-  }
-  // to: the set's place in a stage.  What lies behind the last block is filled with zeros.
-  __device__ __forceinline__ void load(uint32_t to, int64_t tile, int log_rows, const DotsParams &q) const {
+  __device__ __forceinline__ void start(const uint8_t *messages, const PackedRows &ids, const DotsParams &q, int log_rows) {
+    auto message = [&](int r) -> const uint8_t * {
+      const int i = r & (q.rows - 1);
+      return i < ids.n && r >> log_rows < q.segments ? messages + ids.id[i] * q.message_bytes : nullptr;
+    };
     const int c = threadIdx.x & 7;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (row[i] < 0) continue;
-      const int r = i * 16 + (threadIdx.x >> 3);
-      const int64_t block = (tile * q.segments + (r >> log_rows)) * 8 + c;
-      const uint8_t *from = messages + row[i] + block * 16;
-      const bool there = block < q.blocks && access_ok(from, 16);
-      copy_async_16(to + r * 128 + ((c ^ (r & 7)) << 4), there ? from : messages, there ? 16u : 0u);
+    for (int i = 0; i < kPieces; ++i) {
+      const int r = i * (kThreadsOf / 8) + (threadIdx.x >> 3);
+      const uint8_t *m = message(r);
+      block[i] = (int64_t)(r >> log_rows) * 8 + c;
+      codes[i] = m ? m + block[i] * 16 : nullptr;
+      to[i] = r * 128 + ((c ^ (r & 7)) << 4);  // 16-byte pieces change places within a row, the 128-byte swizzle
     }
-    if (own < 0) return;
-    const int r = threadIdx.x;
+    const int r = threadIdx.x & (kDotsRows - 1), g = threadIdx.x / kDotsRows;
+    const uint8_t *m = message(r);
+    scale_block = (int64_t)(r >> log_rows) * 8 + 4 * g;
+    scales = m ? m + q.scales_at + scale_block : nullptr;
+    scales_to = kDotsCodeBytes + g * 512 + (r & 31) * 16 + (r >> 5) * 4;
+  }
+  // at: the set's place in a stage.  What lies behind the last block is filled with zeros.
+  __device__ __forceinline__ void load(uint32_t at, int64_t tile, const DotsParams &q) const {
+    const int64_t first = tile * q.segments * 8;  // block of the tile
+    if (first + q.segments * 8 <= q.blocks) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int64_t block = (tile * q.segments + (r >> log_rows)) * 8 + 4 * g;
-      const uint8_t *from = messages + own + q.scales_at + block;
-      const int64_t left = q.blocks - block;
-      uint32_t bytes = left >= 4 ? 4u : left > 0 ? (uint32_t)left : 0u;
-      if (!access_ok(from, bytes)) bytes = 0;
-      copy_async_4(to + kDotsCodeBytes + g * 512 + (r & 31) * 16 + (r >> 5) * 4, bytes ? from : messages, bytes);
+      for (int i = 0; i < kPieces; ++i)
+        if (codes[i] && access_ok(codes[i] + first * 16, 16)) copy_async_16(at + to[i], codes[i] + first * 16, 16u);
+      if (scales && access_ok(scales + first, 4)) copy_async_4(at + scales_to, scales + first, 4u);
+      return;
     }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      if (!codes[i]) continue;
+      const bool there = first + block[i] < q.blocks && access_ok(codes[i] + first * 16, 16);
+      copy_async_16(at + to[i], there ? codes[i] + first * 16 : codes[i], there ? 16u : 0u);
+    }
+    if (!scales) return;
+    const int64_t left = q.blocks - first - scale_block;
+    uint32_t bytes = left >= 4 ? 4u : left > 0 ? (uint32_t)left : 0u;
+    if (!access_ok(scales + first, bytes)) bytes = 0;
+    copy_async_4(at + scales_to, bytes ? scales + first : scales, bytes);
   }
 };
 
-// partials[pair][block]: 64-bit sums of this block's tiles.
+__device__ __forceinline__ void barrier_init(uint64_t *barrier, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(barrier)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint64_t *barrier) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_address(barrier)) : "memory");
+}
+// The barrier gets an arrival once all products so far are done.
+__device__ __forceinline__ void barrier_commit(uint64_t *barrier) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(barrier))
+               : "memory");
+}
+
+// A ring of tiles in shared memory between the warps that copy and the threads that ask for the products, an accumulator
+// between each of those and the warps that add them up.  partials[pair][block]: 64-bit sums of the block's tiles.
 template <bool kSame>
 __global__ void __launch_bounds__(kDotsThreads)
 k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, double *__restrict__ partials,
               const __grid_constant__ DotsParams q) {
+  using Stages = DotsStages<kSame>;
+  constexpr int kStages = Stages::value;
   extern __shared__ uint8_t shared[];
-  __shared__ __align__(8) uint64_t barriers[kDotsMaxStages];
+  __shared__ __align__(8) uint64_t full[kStages], empty[kStages];
+  __shared__ __align__(8) uint64_t sum_full[kDotsMmaWarps], sum_empty[kDotsMmaWarps];
   __shared__ uint32_t tmem_base;
   __shared__ int failed;
-  constexpr int kSets = kSame ? 1 : 2;
-  constexpr int kStageBytes = kSets * kDotsSetBytes;
-  constexpr int kStages = kSame ? kDotsMaxStages : 4;
   const uint32_t stages_at = (shared_address(shared) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int log_rows = 31 - __clz(q.rows);
-  if (warp == 0) {
+  const int n_tiles = (int)((q.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x);
+  if (warp == kDotsLoadWarps) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&tmem_base)),
                  "n"(kDotsTmemColumns)
                  : "memory");
@@ -406,110 +624,140 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   }
   if (threadIdx.x == 0) {
     failed = 0;
-    for (int i = 0; i < kStages; ++i)
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&barriers[i])) : "memory");
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(&full[i], 32 * kDotsLoadWarps);
+      barrier_init(&empty[i], 1);
+    }
+    for (int i = 0; i < kDotsMmaWarps; ++i) {
+      barrier_init(&sum_full[i], 1);
+      barrier_init(&sum_empty[i], kDotsSumWarps);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  DotsLoader from_a, from_b;
-  from_a.start(a, q.a, q);
-  if (!kSame) from_b.start(b, q.b, q);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base;
-
-  const int n_tiles = (int)((q.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x);
-  auto load = [&](int t) {
-    if (t < n_tiles) {
-      const int64_t tile = blockIdx.x + (int64_t)t * gridDim.x;
-      const uint32_t to = stages_at + (t % kStages) * kStageBytes;
-      from_a.load(to, tile, log_rows, q);
-      if (!kSame) from_b.load(to + kDotsSetBytes, tile, log_rows, q);
-    }
-    copy_async_commit();
-  };
-  // Tile t's stage takes tile t + kStages once the products of tile t are done; they are asked for two tiles later, when
-  // they are (so that kStages - 2 tiles are in flight).
-  constexpr int kAhead = kStages - 2;
-  for (int t = 0; t < kAhead; ++t) load(t);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   double sum[32];
+
+  if (warp < kDotsLoadWarps) {
+    DotsLoader from_a, from_b;
+    from_a.start(a, q.a, q, log_rows);
+    if (!kSame) from_b.start(b, q.b, q, log_rows);
+    for (int t = 0; t < n_tiles; ++t) {
+      // The stage's last tile was t - kStages; its products are done.
+      if (t >= kStages && !barrier_wait(&empty[t % kStages], (t / kStages - 1) & 1)) {
+        failed = 1;
+        break;
+      }
+      const int64_t tile = blockIdx.x + (int64_t)t * gridDim.x;
+      const uint32_t to = stages_at + (t % kStages) * Stages::bytes;
+      from_a.load(to, tile, q);
+      if (!kSame) from_b.load(to + kDotsSetBytes, tile, q);
+      copy_async_arrive(&full[t % kStages]);
+    }
+    copy_async_wait_all();
+  } else if (warp < kDotsLoadWarps + kDotsSumWarps) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) sum[i] = 0.0;
-  int in_sum = 0;
-  for (int t = 0; t < n_tiles; ++t) {
-    if (t >= 2 && !barrier_wait(shared_address(&barriers[(t - 2) % kStages]), ((t - 2) / kStages) & 1)) failed = 1;
-    load(t + kAhead);
-    copy_async_wait<kAhead>();
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
-    if (failed) break;
-    if (threadIdx.x == 0) {
+    for (int i = 0; i < 32; ++i) sum[i] = 0.0;
+    // Row r needs columns r / R * R .. + R - 1: they lie among the 32 of its warp's rows.
+    const uint32_t rows = (warp - kDotsLoadWarps) * 32;
+    const int n_sums = (n_tiles + kDotsMmaWarps * kDotsFlush - 1) / (kDotsMmaWarps * kDotsFlush);
+    for (int f = 0; f < n_sums; ++f) {
+      for (int m = 0; m < kDotsMmaWarps; ++m) {
+        if (n_tiles <= m + f * kDotsMmaWarps * kDotsFlush) break;
+        if (!barrier_wait(&sum_full[m], f & 1)) failed = 1;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        float v[32];
+        tmem_load_32(tmem + (rows << 16) + m * kDotsRows + rows, v);
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) barrier_arrive(&sum_empty[m]);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum[i] += (double)v[i];
+      }
+      if (failed) break;
+    }
+  } else if (lane == 0) {
+    // Warp m takes the tiles t = m, m + kDotsMmaWarps, ...: what one tile has to wait for (its copies, the fence, its
+    // scales) passes under the products of another.
+    const int m = warp - kDotsLoadWarps - kDotsSumWarps;
+    const uint32_t accumulator = tmem + m * kDotsRows;
+    int in_sum = 0, f = 0;
+    for (int t = m; t < n_tiles; t += kDotsMmaWarps) {
+      if (in_sum == 0 && f > 0 && !barrier_wait(&sum_empty[m], (f - 1) & 1)) {
+        failed = 1;
+        break;
+      }
+      const int stage = t % kStages;
+      if (!barrier_wait(&full[stage], (t / kStages) & 1)) {
+        failed = 1;
+        break;
+      }
+      // The copies were made through the generic proxy, the tensor core reads through the asynchronous one.  (The threads
+      // that copy would wait here for all their copies in flight.)
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t stage = stages_at + (t % kStages) * kStageBytes;
-      const uint32_t stage_b = kSame ? stage : stage + kDotsSetBytes;
-      const uint32_t scales = tmem + 128 + (t & 1) * 16;  // not those that the tile before still uses
+      const uint32_t at = stages_at + stage * Stages::bytes, at_b = kSame ? at : at + kDotsSetBytes;
+      // The scales have a place per stage: it is free when the stage is.
+      const uint32_t scales = tmem + kDotsMmaWarps * kDotsRows + stage * (kSame ? 8 : 16);
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        scales_to_tmem(scales + 4 * g, stage + kDotsCodeBytes + g * 512);
-        if (!kSame) scales_to_tmem(scales + 8 + 4 * g, stage_b + kDotsCodeBytes + g * 512);
+        scales_to_tmem(scales + 4 * g, at + kDotsCodeBytes + g * 512);
+        if (!kSame) scales_to_tmem(scales + 8 + 4 * g, at_b + kDotsCodeBytes + g * 512);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t scales_a = scales + 4 * (k / 2), scales_b = kSame ? scales_a : scales_a + 8;
-        dots_mma(tmem, codes_descriptor(stage + 32 * k), codes_descriptor(stage_b + 32 * k), scales_a, scales_b, k & 1,
+        dots_mma(accumulator, codes_descriptor(at + 32 * k), codes_descriptor(at_b + 32 * k), scales_a, scales_b, k & 1,
                  in_sum > 0 || k > 0);
       }
-      asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                       shared_address(&barriers[t % kStages]))
-                   : "memory");
-    }
-    if (++in_sum == kDotsFlush || t + 1 == n_tiles) {
-      if (!barrier_wait(shared_address(&barriers[t % kStages]), (t / kStages) & 1)) failed = 1;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      // Row r needs columns r / R * R .. + R - 1: they lie among the 32 of its warp's rows.
-      float v[32];
-      tmem_load_32(tmem + ((uint32_t)(warp * 32) << 16) + warp * 32, v);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) sum[i] += (double)v[i];
-      in_sum = 0;
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncthreads();
-      if (failed) break;
+      barrier_commit(&empty[stage]);
+      if (++in_sum == kDotsFlush || t + kDotsMmaWarps >= n_tiles) {
+        barrier_commit(&sum_full[m]);
+        in_sum = 0;
+        ++f;
+      }
     }
   }
-  copy_async_wait<0>();
-  if (failed) barrier_wait(shared_address(&barriers[(n_tiles - 1) % kStages]), ((n_tiles - 1) / kStages) & 1);
   __syncthreads();
-  // The blocks on the diagonal, segment by segment, in the stages' place.
+  // The blocks on the diagonal, [segment][j][i], in the stages' place (whose last products are in the sums).
   double *mine = reinterpret_cast<double *>(shared + (stages_at - shared_address(shared)));
-  const int row_in = threadIdx.x & (q.rows - 1), segment = threadIdx.x >> log_rows;
+  if (warp >= kDotsLoadWarps && warp < kDotsLoadWarps + kDotsSumWarps) {
+    const int r = threadIdx.x - 32 * kDotsLoadWarps, i = r & (q.rows - 1), s = r >> log_rows;
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if ((i >> log_rows) == (lane >> log_rows)) mine[((segment << log_rows) + row_in << log_rows) + (i & (q.rows - 1))] = sum[i];
+    for (int c = 0; c < 32; ++c)
+      if ((c >> log_rows) == (lane >> log_rows)) mine[(((s << log_rows) + (c & (q.rows - 1))) << log_rows) + i] = sum[c];
+  }
   __syncthreads();
-  const int pairs = q.a.n * q.b.n;
-  for (int p = threadIdx.x; p < pairs; p += kDotsThreads) {
-    const int i = p / q.b.n, j = p - i * q.b.n;
-    if (kSame && i > j) continue;
+  // A lane has every `lanes`-th segment of a pair, four of them; then a butterfly over a pair's lanes.
+  const int log_lanes = min(5, 5 - log_rows), per_warp = 32 >> log_lanes, part = lane >> (5 - log_lanes);
+  const int all = q.rows << log_rows;
+  for (int e0 = warp * per_warp; e0 < all; e0 += kDotsThreads / 32 * per_warp) {
+    const int e = e0 + (lane & (per_warp - 1)), i = e & (q.rows - 1), j = e >> log_rows;
     double total = 0.0;
-    for (int s = 0; s < q.segments; ++s) total += mine[((s << log_rows) + i << log_rows) + j];
+    for (int s = part; s < q.segments; s += 1 << log_lanes) total += mine[(s << (2 * log_rows)) + e];
+    for (int off = 16; off >= per_warp; off >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, off);
+    if (part || i >= q.a.n || j >= q.b.n || (kSame && i > j)) continue;
     // A wait that ran out (which nothing is known to cause) shows as products that are no numbers.
-    double *at = partials + (int64_t)p * gridDim.x + blockIdx.x;
+    double *at = partials + (int64_t)(i * q.b.n + j) * gridDim.x + blockIdx.x;
     if (access_ok(at, 8)) *at = failed ? __longlong_as_double(0x7FF8000000000000ll) : total;
   }
-  if (warp == 0)
+  if (warp == kDotsLoadWarps)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kDotsTmemColumns) : "memory");
 }
 
 // out[pair] = sum of the blocks' partial sums in a fixed order, a warp per pair; of a set with itself each sum is for two.
+// Launched while k_packed_dots runs, so that its start is not waited for after that.
 __global__ void __launch_bounds__(kThreads)
 k_packed_dots_finish(const double *__restrict__ partials, int n_blocks, int m, int n, int same, float *__restrict__ out) {
   const int p = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (p >= m * n) return;
   const int i = p / n, j = p - i * n;
-  if (same && i > j) return;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (p >= m * n || (same && i > j)) return;
   double sum = 0.0;
-  for (int k = lane; k < n_blocks; k += 32) sum += partials[(int64_t)p * n_blocks + k];
+  for (int k = lane; k < n_blocks; k += 32) sum += __ldcg(partials + (int64_t)p * n_blocks + k);
   sum = warp_sum(sum);
   if (lane) return;
   if (access_ok(out + p, 4)) out[p] = (float)sum;
