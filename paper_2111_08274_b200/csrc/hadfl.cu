@@ -1178,9 +1178,10 @@ int hadfl_pack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const void
   DeviceGuard guard(h->device);
   if (!exchange_buffers(h, base, residual, messages)) return HADFL_ERR_INVALID;
   HADFL_KEEP(h, base, residual, messages);
-  launch_pack(packed_shape(h), packed_rows(device_ids, n), base, residual, rounding == HADFL_ROUND_STOCHASTIC,
-              (uint64_t)round, h->keys, (uint8_t *)messages);
-  return check_launch(h);
+  HADFL_CUDA(h, launch_pack(packed_shape(h), packed_rows(device_ids, n), base, residual,
+                            rounding == HADFL_ROUND_STOCHASTIC, (uint64_t)round, h->keys, (uint8_t *)messages));
+  ++h->launches;
+  return HADFL_OK;
 }
 
 int hadfl_unpack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const void *base, const void *messages) {
@@ -1188,8 +1189,9 @@ int hadfl_unpack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const vo
   DeviceGuard guard(h->device);
   if (!exchange_buffers(h, base, nullptr, messages)) return HADFL_ERR_INVALID;
   HADFL_KEEP(h, base, nullptr, messages);
-  launch_unpack(packed_shape(h), packed_rows(device_ids, n), base, (const uint8_t *)messages);
-  return check_launch(h);
+  HADFL_CUDA(h, launch_unpack(packed_shape(h), packed_rows(device_ids, n), base, (const uint8_t *)messages));
+  ++h->launches;
+  return HADFL_OK;
 }
 
 int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, const double *versions, void *base,
@@ -1210,10 +1212,9 @@ int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, 
   scaled_versions(h, versions, x);
   aggregation_weights(h->cfg.weight_mode, x, h->avail, h->cfg.n_devices, selected, k, from.a);
   for (int j = 0; j < k; ++j) from.id[j] = selected[j];
-  launch_aggregate_packed(packed_shape(h), from, packed_rows(dst_ids, n), base, move_base != 0,
-                          (const uint8_t *)messages);
-  const int rc = check_launch(h);
-  if (rc != HADFL_OK) return rc;
+  HADFL_CUDA(h, launch_aggregate_packed(packed_shape(h), from, packed_rows(dst_ids, n), base, move_base != 0,
+                                        (const uint8_t *)messages));
+  ++h->launches;
   uint32_t vmax = 0;
   for (int j = 0; j < k; ++j) vmax = h->version[selected[j]] > vmax ? h->version[selected[j]] : vmax;
   for (int j = 0; j < n; ++j) h->version[dst_ids[j]] = vmax;
@@ -1250,7 +1251,8 @@ int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const vo
 #endif
   HADFL_CUDA(h, launch_packed_dots(packed_shape(h), packed_rows(a_ids, m), (const uint8_t *)a_messages,
                                    packed_rows(b_ids, n), (const uint8_t *)b_messages, out, h->d_dots));
-  return check_launch(h);
+  h->launches += 2;
+  return HADFL_OK;
 }
 
 int hadfl_set_sync_beta(hadfl_handle *h, float beta) {

@@ -37,6 +37,26 @@ unsigned column_blocks(bool bf16, int64_t columns) {
   return (unsigned)((columns + per_block - 1) / per_block);
 }
 
+// A launch whose blocks may become resident while the kernel before it in the stream still runs (they wait for it
+// themselves, see wait_for_stream): the start of a kernel passes under the end of the one before.  Measured, us, launches
+// one after the other / so: products of 4 messages of 100,000 parameters 6.1 / 4.9, of 8 of 11.2 M 14.9 / 13.5; aggregate 4
+// fp32 devices of 11.2 M 42.6 / 41.8, read the same 34.3 / 33.5.
+template <typename... Params, typename... Args>
+cudaError_t launch_dependent(void (*kernel)(Params...), unsigned grid, int threads, size_t shared_bytes, cudaStream_t stream,
+                             Args... args) {
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3(grid);
+  config.blockDim = dim3((unsigned)threads);
+  config.dynamicSmemBytes = shared_bytes;
+  config.stream = stream;
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, kernel, static_cast<Params>(args)...);
+}
+
 bool at_32(const void *p) { return ((uintptr_t)p & 31u) == 0; }
 
 // The rows of a pack or unpack launch, and how many of them a block walks over: all, so that the base is loaded once, but
@@ -62,7 +82,7 @@ unsigned split_rows(const PackedShape &s, const PackedRows &rows, int64_t column
 
 }  // namespace
 
-void launch_pack(const PackedShape &s, const PackedRows &rows, const void *base, float *residual, bool stochastic,
+cudaError_t launch_pack(const PackedShape &s, const PackedRows &rows, const void *base, float *residual, bool stochastic,
                  uint64_t round, const PhiloxKeys &keys, uint8_t *messages) {
   PackParams q;
   const int64_t scales_at = packed_scales_at(s.n_params);
@@ -76,6 +96,7 @@ void launch_pack(const PackedShape &s, const PackedRows &rows, const void *base,
     const uint64_t p0 = (uint64_t)kPhiloxM0 * ((uint32_t)(p1 >> 32) ^ (uint32_t)round ^ keys.a[0]);
     q.random[j] = RowRandom{(uint32_t)p1 ^ keys.a[1], (uint32_t)(p0 >> 32) ^ keys.b[1], (uint32_t)p0};
   }
+  cudaError_t rc = cudaSuccess;
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;
     with_flag(base != nullptr, [&](auto has_base) {
@@ -83,30 +104,33 @@ void launch_pack(const PackedShape &s, const PackedRows &rows, const void *base,
         with_flag(stochastic, [&](auto is_stochastic) {
           with_flag(at_32(residual), [&](auto is_at_32) {
             if constexpr (has_residual.value || is_at_32.value)  // without a residual there are no stores to rows
-              k_pack<WT, has_base.value, has_residual.value, is_stochastic.value, is_at_32.value>
-                  <<<grid, kThreads, 0, s.stream>>>((const WT *)s.w, (const WT *)base, residual, messages, keys, q);
+              rc = launch_dependent(k_pack<WT, has_base.value, has_residual.value, is_stochastic.value, is_at_32.value>, grid,
+                                    kThreads, 0, s.stream, (const WT *)s.w, (const WT *)base, residual, messages, keys, q);
           });
         });
       });
     });
   });
+  return rc;
 }
 
-void launch_unpack(const PackedShape &s, const PackedRows &rows, const void *base, const uint8_t *messages) {
+cudaError_t launch_unpack(const PackedShape &s, const PackedRows &rows, const void *base, const uint8_t *messages) {
   UnpackParams q;
   const unsigned grid = split_rows(s, rows, s.n_params, q);
+  cudaError_t rc = cudaSuccess;
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;
     with_flag(base != nullptr, [&](auto has_base) {
       with_flag(at_32(s.w) && s.stride % (int64_t)(32 / sizeof(WT)) == 0, [&](auto is_at_32) {
-        k_unpack<WT, has_base.value, is_at_32.value><<<grid, kThreads, 0, s.stream>>>((WT *)s.w, (const WT *)base, messages,
-                                                                                     q);
+        rc = launch_dependent(k_unpack<WT, has_base.value, is_at_32.value>, grid, kThreads, 0, s.stream, (WT *)s.w,
+                              (const WT *)base, messages, q);
       });
     });
   });
+  return rc;
 }
 
-void launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights, const PackedRows &receivers, void *base,
+cudaError_t launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights, const PackedRows &receivers, void *base,
                              bool move_base, const uint8_t *messages) {
   AggregateParams q;
   q.k = weights.k;
@@ -120,15 +144,17 @@ void launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights,
   }
   for (int j = 0; j < q.n; ++j) q.row_at[j] = receivers.id[j] * s.stride;
   const unsigned grid = column_blocks(s.bf16, s.n_params);
+  cudaError_t rc = cudaSuccess;
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;
     with_flag(base != nullptr, [&](auto has_base) {
       with_flag(at_32(s.w) && at_32(base) && s.stride % (int64_t)(32 / sizeof(WT)) == 0, [&](auto is_at_32) {
-        k_aggregate_packed<WT, has_base.value, is_at_32.value><<<grid, kThreads, 0, s.stream>>>((WT *)s.w, (WT *)base,
-                                                                                               messages, q);
+        rc = launch_dependent(k_aggregate_packed<WT, has_base.value, is_at_32.value>, grid, kThreads, 0, s.stream, (WT *)s.w,
+                              (WT *)base, messages, q);
       });
     });
   });
+  return rc;
 }
 
 size_t packed_dots_scratch_bytes(int sm_count) {
@@ -159,20 +185,11 @@ cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, c
     auto kernel = k_packed_dots<is_same.value>;
     const int bytes = 1024 + Stages::value * Stages::bytes;
     rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (rc == cudaSuccess) kernel<<<blocks, kDotsThreads, bytes, s.stream>>>(a, b, partials, q);
+    if (rc == cudaSuccess) rc = launch_dependent(kernel, (unsigned)blocks, kDotsThreads, bytes, s.stream, a, b, partials, q);
   });
   if (rc != cudaSuccess) return rc;
-  cudaLaunchConfig_t config = {};
-  config.gridDim = dim3((unsigned)((pairs + kThreads / 32 - 1) / (kThreads / 32)));
-  config.blockDim = dim3(kThreads);
-  config.stream = s.stream;
-  cudaLaunchAttribute early;
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  config.attrs = &early;
-  config.numAttrs = 1;
-  return cudaLaunchKernelEx(&config, k_packed_dots_finish, (const double *)partials, blocks, (int)a_rows.n, (int)b_rows.n,
-                            (int)same, out);
+  return launch_dependent(k_packed_dots_finish, (unsigned)((pairs + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0,
+                          s.stream, (const double *)partials, blocks, (int)a_rows.n, (int)b_rows.n, (int)same, out);
 }
 
 #ifdef HADFL_DEBUG

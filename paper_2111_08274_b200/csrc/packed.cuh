@@ -19,6 +19,13 @@ namespace hadfl {
 
 constexpr uint32_t kPackedNan = 255;
 
+// The kernels here are launched as dependents of what is before them in the stream (launch_dependent): their blocks may
+// become resident while the kernel before still runs, and touch no memory before this.  It returns when that kernel is
+// done and its writes are visible; as every kernel here begins with it, so is everything before that.
+__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The kernel behind this one may become resident once all blocks are here.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Parameters per thread, in parts of 8.
 template <typename WT>
 struct PackedE {
@@ -183,6 +190,8 @@ k_pack(const WT *__restrict__ w, const WT *base, float *__restrict__ residual, u
   const int64_t block = blockIdx.x / q.row_blocks;
   const int64_t group = block * kThreads + threadIdx.x;
   const int64_t column = E * group;
+  let_next_start();
+  wait_for_stream();
   if (column >= q.scale_columns) return;  // whole warps: scale_columns is a multiple of 32 * 128
   const int first = blockIdx.x % q.row_blocks * q.rows_per_block;
   const int end = min(first + q.rows_per_block, q.n);
@@ -350,6 +359,8 @@ k_unpack(WT *w, const WT *base, const uint8_t *__restrict__ messages, const __gr
   const int64_t column = E * (block * kThreads + threadIdx.x);
   const int first = blockIdx.x % q.row_blocks * q.rows_per_block;
   const int end = min(first + q.rows_per_block, q.n);
+  let_next_start();
+  wait_for_stream();
   if (column >= q.n_params) return;
   with_live<E>(q.n_params, block, [&](auto live) {
     RawParts<WT, kParts> base_raw;
@@ -393,6 +404,8 @@ k_aggregate_packed(WT *w, WT *base, const uint8_t *__restrict__ messages, const 
   constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, B = kPackedBatch;
   const int64_t block = blockIdx.x;
   const int64_t column = E * (block * kThreads + threadIdx.x);
+  let_next_start();
+  wait_for_stream();
   if (column >= q.n_params) return;
   with_live<E>(q.n_params, block, [&](auto live) {
     RawParts<WT, kParts> base_raw;
@@ -622,7 +635,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (threadIdx.x == 0) {
+  if (warp == kDotsLoadWarps + 1 && lane == 0) {
     failed = 0;
     for (int i = 0; i < kStages; ++i) {
       barrier_init(&full[i], 32 * kDotsLoadWarps);
@@ -634,27 +647,35 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  DotsLoader from_a, from_b;
+  auto load = [&](int t) {
+    const int64_t tile = blockIdx.x + (int64_t)t * gridDim.x;
+    const uint32_t to = stages_at + (t % kStages) * Stages::bytes;
+    from_a.load(to, tile, q);
+    if (!kSame) from_b.load(to + kDotsSetBytes, tile, q);
+  };
+  if (warp < kDotsLoadWarps) {
+    from_a.start(a, q.a, q, log_rows);
+    if (!kSame) from_b.start(b, q.b, q, log_rows);
+    wait_for_stream();
+    load(0);
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  let_next_start();  // with the tensor memory allocated: a block of the next call waits for it without a place on this SM
   double sum[32];
 
   if (warp < kDotsLoadWarps) {
-    DotsLoader from_a, from_b;
-    from_a.start(a, q.a, q, log_rows);
-    if (!kSame) from_b.start(b, q.b, q, log_rows);
-    for (int t = 0; t < n_tiles; ++t) {
+    copy_async_arrive(&full[0]);
+    for (int t = 1; t < n_tiles; ++t) {
       // The stage's last tile was t - kStages; its products are done.
       if (t >= kStages && !barrier_wait(&empty[t % kStages], (t / kStages - 1) & 1)) {
         failed = 1;
         break;
       }
-      const int64_t tile = blockIdx.x + (int64_t)t * gridDim.x;
-      const uint32_t to = stages_at + (t % kStages) * Stages::bytes;
-      from_a.load(to, tile, q);
-      if (!kSame) from_b.load(to + kDotsSetBytes, tile, q);
+      load(t);
       copy_async_arrive(&full[t % kStages]);
     }
     copy_async_wait_all();
@@ -722,6 +743,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
     }
   }
   __syncthreads();
+  wait_for_stream();  // (done long since) what follows writes where the call before may have read
   // The blocks on the diagonal, [segment][j][i], in the stages' place (whose last products are in the sums).
   double *mine = reinterpret_cast<double *>(shared + (stages_at - shared_address(shared)));
   if (warp >= kDotsLoadWarps && warp < kDotsLoadWarps + kDotsSumWarps) {
@@ -749,12 +771,12 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
 }
 
 // out[pair] = sum of the blocks' partial sums in a fixed order, a warp per pair; of a set with itself each sum is for two.
-// Launched while k_packed_dots runs, so that its start is not waited for after that.
 __global__ void __launch_bounds__(kThreads)
 k_packed_dots_finish(const double *__restrict__ partials, int n_blocks, int m, int n, int same, float *__restrict__ out) {
   const int p = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int i = p / n, j = p - i * n;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  let_next_start();
+  wait_for_stream();
   if (p >= m * n || (same && i > j)) return;
   double sum = 0.0;
   for (int k = lane; k < n_blocks; k += 32) sum += __ldcg(partials + (int64_t)p * n_blocks + k);

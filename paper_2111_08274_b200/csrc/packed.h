@@ -44,10 +44,10 @@ struct PackedWeights {
   float a[kPackedMaxRows];
 };
 
-void launch_pack(const PackedShape &s, const PackedRows &rows, const void *base, float *residual, bool stochastic,
+cudaError_t launch_pack(const PackedShape &s, const PackedRows &rows, const void *base, float *residual, bool stochastic,
                  uint64_t round, const PhiloxKeys &keys, uint8_t *messages);
-void launch_unpack(const PackedShape &s, const PackedRows &rows, const void *base, const uint8_t *messages);
-void launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights, const PackedRows &receivers, void *base,
+cudaError_t launch_unpack(const PackedShape &s, const PackedRows &rows, const void *base, const uint8_t *messages);
+cudaError_t launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights, const PackedRows &receivers, void *base,
                              bool move_base, const uint8_t *messages);
 // out[i * b_rows.n + j] = sum over the parameters of message a_rows.id[i] of a times message b_rows.id[j] of b.
 // scratch: packed_dots_scratch_bytes() bytes.
