@@ -202,7 +202,8 @@ int debug_error(uint64_t *addr) {
 // Buffers that callers hand to a call, which may still run when it returns, and again in a captured graph: they stay
 // in the table, the oldest making room.
 int debug_keep(const void *p, size_t nbytes) {
-  static const void *kept[kDebugRanges / 2];
+  constexpr int kKept = 16;
+  static const void *kept[kKept];
   static int next = 0;
   const uint64_t at = (uint64_t)(uintptr_t)p;
   for (int r = 0; r < g_debug_host.n; ++r)
@@ -210,7 +211,7 @@ int debug_keep(const void *p, size_t nbytes) {
   cudaDeviceSynchronize();
   debug_remove(kept[next]);
   kept[next] = p;
-  next = (next + 1) % (kDebugRanges / 2);
+  next = (next + 1) % kKept;
   debug_add(p, nbytes);
   return debug_publish();
 }

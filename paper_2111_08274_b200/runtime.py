@@ -57,6 +57,16 @@ class Arena:
         steps = np.stack([wl.steps_for_round(first_round + i) for i in range(n_rounds)])
         return self.h.rounds(first_round, steps, wl.lr, wl.k, self.select_seed, wl.sync_every)
 
+    def run_round_packed(self, r, exchange, versions=None):
+        """A round whose devices exchange messages of 4 bits per parameter (see Exchange) instead of models, as separate
+        calls.  Returns the selected ids (draw order); exchange.products holds the products of their messages."""
+        wl, h = self.wl, self.h
+        h.local_step(self.ids, wl.steps_for_round(r), wl.lr)
+        sel = h.select(r, wl.k, self.select_seed, versions)
+        exchange.synchronise(sel, r, bool(wl.sync_every) and (r + 1) % wl.sync_every == 0, versions)
+        h.stats_enqueue(int(sel[0]))
+        return sel
+
     def run_round(self, r, stats=True):
         """One round of the hot path as separate calls: local steps of every device, selection,
         aggregation with write-back (plus, on the workload's global-synchronisation rounds, the
@@ -74,3 +84,41 @@ class Arena:
         if stats:
             h.stats_enqueue(int(sel[0]))
         return sel
+
+
+class Exchange:
+    """What the devices of an arena need to send each other messages of 4 bits per parameter: the messages, the base that
+    all devices have in common (device 0's model when this is made, in a new arena the initial model of all; then each
+    model that a global synchronisation has sent to all of them) and, per device, the residual that its messages have
+    left out so far.
+
+    rounding: binding.ROUND_* of the messages.  residual=False sends every update by itself."""
+
+    def __init__(self, arena, rounding=binding.ROUND_STOCHASTIC, residual=True):
+        wl = arena.wl
+        self.arena, self.rounding = arena, rounding
+        with torch.cuda.stream(arena.stream):
+            self.messages = torch.zeros((wl.n_devices, binding.hadfl_packed_bytes(wl.n_params)), dtype=torch.uint8,
+                                        device=arena.device)
+            self.base = arena.w[0, :wl.n_params].clone()
+            self.residual = torch.zeros((wl.n_devices, arena.stride), device=arena.device) if residual else None
+            self.products = torch.zeros((wl.k, wl.k), device=arena.device)
+
+    def synchronise(self, selected, r, to_all=False, versions=None):
+        """Round r's partial aggregation (Eq. 5) from the selected devices' messages, and with to_all the global
+        synchronisation: an overwrite moves the base to the aggregate; a mix (the workload's sync_beta below 1) leaves
+        the devices with different models, and the base as it is."""
+        h, wl, messages, base = self.arena.h, self.arena.wl, self.messages.data_ptr(), self.base.data_ptr()
+        h.pack(selected, messages, base_ptr=base, residual_ptr=None if self.residual is None else self.residual.data_ptr(),
+               rounding=self.rounding, round_=r)
+        overwrite = to_all and wl.sync_beta == 1.0
+        h.aggregate_packed(selected, messages, base_ptr=base, dst_ids=self.arena.ids if overwrite else None,
+                           move_base=overwrite, versions=versions)
+        if to_all and not overwrite:
+            h.integrate(int(selected[0]), np.setdiff1d(self.arena.ids, selected).astype(np.int32), wl.sync_beta)
+        h.packed_dots(selected, messages, self.products.data_ptr())
+
+    def read_products(self):
+        """Scalar products of the last messages, [k, k] in draw order (synchronises)."""
+        self.arena.stream.synchronize()
+        return self.products.cpu().numpy()
