@@ -306,8 +306,8 @@ int hadfl_unpack(hadfl_handle *h, const int32_t *device_ids, int32_t n, const vo
  *     acc = a_0 * d_0;  acc = fma(a_j, d_j, acc), j = 1..k-1;  w[dst_ids[i]] = base + acc for all i
  * d_j the message of selected[j], a_j as in hadfl_aggregate (from `versions`, NULL = the handle's counters).
  * dst_ids: the n receivers (distinct); n = 0 and dst_ids = NULL: the selected devices.  move_base != 0: the
- * base becomes the aggregate too (base must not be NULL), as it may when all devices receive it.  Momentum is
- * not touched.  Every receiver takes the largest version among the selected devices.  One kernel. */
+ * base becomes the aggregate too (base must not be NULL, nor the row of a device that is no receiver), as it
+ * may when all devices receive it.  Momentum is not touched.  Every receiver takes the largest version among the selected devices.  One kernel. */
 int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, const double *versions, void *base,
                            int32_t move_base, const int32_t *dst_ids, int32_t n, const void *messages);
 
@@ -316,7 +316,9 @@ int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, 
  * = NULL (n = 0): the second set is the first, and out the m x m matrix of its products, which gives the norm of
  * every update and the angle and distance of every two (hadfl_stats: the distances to one replica).
  * out: DEVICE pointer to floats, 4-byte aligned.  A message with a block that reads as NaN has NaN products.
- * Deterministic: fixed grid and summation order. */
+ * Products of single parameters and their sums over 2^14 and more of them are fp32 (and overflow as such), the
+ * sums of those have 64 bits.  Deterministic: fixed grid and summation order.  The partial sums lie in memory of the
+ * handle: graphs that hold this call of one handle are not to run at the same time. */
 int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const void *a_messages, const int32_t *b_ids,
                       int32_t n, const void *b_messages, float *out);
 

@@ -20,7 +20,7 @@ HADFL_HD bool range_holds(uint64_t lo, uint64_t hi, uint64_t addr, uint64_t nbyt
   return lo <= hi && addr >= lo && addr <= hi && nbytes <= hi - addr;
 }
 
-constexpr int kDebugRanges = 64;
+constexpr int kDebugRanges = 96;
 
 struct DebugRanges {
   uint64_t lo[kDebugRanges], hi[kDebugRanges];

@@ -173,12 +173,43 @@ RowStep row_step(const hadfl_handle *h, int dev, uint64_t base, int steps) {
 #ifdef HADFL_DEBUG
 DebugRanges g_debug_host;
 
+// Buffers that callers hand to a call, which may still run when it returns, and again in a captured graph: they stay
+// in the table behind the handles' ranges; the one that was not used for the longest time makes room.
+struct DebugKept {
+  uint64_t lo, hi, used;
+};
+constexpr int kDebugKept = 16;
+DebugKept g_debug_kept[kDebugKept];
+
 int debug_publish() {
+  DebugRanges t = g_debug_host;
+  for (const DebugKept &k : g_debug_kept) {
+    if (!k.used || t.n >= kDebugRanges) continue;
+    t.lo[t.n] = k.lo;
+    t.hi[t.n] = k.hi;
+    ++t.n;
+  }
   const size_t bytes = offsetof(DebugRanges, error);
-  return cudaMemcpyToSymbol(g_debug, &g_debug_host, bytes) == cudaSuccess ? packed_debug_publish(&g_debug_host, bytes) : 1;
+  return cudaMemcpyToSymbol(g_debug, &t, bytes) == cudaSuccess ? packed_debug_publish(&t, bytes) : 1;
+}
+int debug_keep(const void *p, size_t nbytes) {
+  static uint64_t now = 0;
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  ++now;
+  DebugKept *oldest = g_debug_kept;
+  for (DebugKept &k : g_debug_kept) {
+    if (k.used && range_holds(k.lo, k.hi, at, nbytes)) {
+      k.used = now;
+      return 0;
+    }
+    if (k.used < oldest->used) oldest = &k;
+  }
+  *oldest = DebugKept{at, at + nbytes, now};
+  cudaDeviceSynchronize();
+  return debug_publish();
 }
 void debug_add(const void *p, size_t nbytes) {
-  if (!p || nbytes == 0 || g_debug_host.n >= kDebugRanges) return;
+  if (!p || nbytes == 0 || g_debug_host.n >= kDebugRanges - kDebugKept) return;
   g_debug_host.lo[g_debug_host.n] = (uint64_t)(uintptr_t)p;
   g_debug_host.hi[g_debug_host.n] = (uint64_t)(uintptr_t)p + nbytes;
   ++g_debug_host.n;
@@ -198,22 +229,6 @@ int debug_error(uint64_t *addr) {
   if (cudaMemcpyFromSymbol(&now, g_debug, sizeof(now)) != cudaSuccess) return 1;
   if (addr) *addr = now.bad_addr;
   return packed_debug_error(addr) || now.error ? 1 : 0;
-}
-// Buffers that callers hand to a call, which may still run when it returns, and again in a captured graph: they stay
-// in the table, the oldest making room.
-int debug_keep(const void *p, size_t nbytes) {
-  constexpr int kKept = 16;
-  static const void *kept[kKept];
-  static int next = 0;
-  const uint64_t at = (uint64_t)(uintptr_t)p;
-  for (int r = 0; r < g_debug_host.n; ++r)
-    if (range_holds(g_debug_host.lo[r], g_debug_host.hi[r], at, nbytes)) return 0;
-  cudaDeviceSynchronize();
-  debug_remove(kept[next]);
-  kept[next] = p;
-  next = (next + 1) % kKept;
-  debug_add(p, nbytes);
-  return debug_publish();
 }
 #define HADFL_DEBUG_RESULT()                            \
   do {                                                   \
@@ -878,7 +893,7 @@ int hadfl_init(const hadfl_config *cfg, hadfl_handle **out) {
   HADFL_CUDA(h, cudaMalloc((void **)&h->d_round_ticket, sizeof(unsigned int) * (1 + n_groups)));
   HADFL_CUDA(h, cudaMemsetAsync(h->d_round_ticket, 0, sizeof(unsigned int) * (1 + n_groups),
                                 h->stream));
-  HADFL_CUDA(h, cudaMalloc(&h->d_dots, packed_dots_scratch_bytes(h->sm_count)));
+  HADFL_CUDA(h, cudaMalloc(&h->d_dots, packed_dots_scratch_bytes(h->sm_count, cfg->n_devices, cfg->n_params)));
   HADFL_CUDA(h, cudaMemsetAsync(h->d_ticket, 0, sizeof(unsigned int), h->stream));
 #ifdef HADFL_DEBUG
   debug_add(h->w, elems * elem_size(h));
@@ -888,7 +903,7 @@ int hadfl_init(const hadfl_config *cfg, hadfl_handle **out) {
   debug_add(h->stats_host, stats_bytes);
   debug_add(h->d_round_partials, sizeof(double) * round_vals * (size_t)scratch_grid);
   debug_add(h->d_round_group_partials, sizeof(double) * round_vals * n_groups);
-  debug_add(h->d_dots, packed_dots_scratch_bytes(h->sm_count));
+  debug_add(h->d_dots, packed_dots_scratch_bytes(h->sm_count, cfg->n_devices, cfg->n_params));
   HADFL_CUDA(h, cudaDeviceSynchronize());
   if (debug_publish()) return HADFL_ERR_CUDA;
 #endif
@@ -1123,6 +1138,10 @@ bool device_buffer(const hadfl_handle *h, const void *p, size_t align) {
   return (at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged) && at.device == h->device;
 }
 
+const void *row_of(const hadfl_handle *h, int32_t id) {
+  return (const char *)h->w + (size_t)id * (size_t)h->stride * elem_size(h);
+}
+
 // The buffers of an exchange call, as the header says.
 bool exchange_buffers(const hadfl_handle *h, const void *base, const void *residual, const void *messages) {
   const size_t n = (size_t)h->cfg.n_devices, row = (size_t)h->stride * elem_size(h);
@@ -1205,6 +1224,12 @@ int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, 
   if (!distinct_ids(h, dst_ids, n)) return HADFL_ERR_INVALID;
   DeviceGuard guard(h->device);
   if (!exchange_buffers(h, base, nullptr, messages)) return HADFL_ERR_INVALID;
+  if (move_base) {  // a device's parameters change with its version only
+    bool is_row = false, is_receiver = false;
+    for (int i = 0; i < h->cfg.n_devices; ++i) is_row |= base == row_of(h, i);
+    for (int j = 0; j < n; ++j) is_receiver |= base == row_of(h, dst_ids[j]);
+    if (is_row && !is_receiver) return HADFL_ERR_INVALID;
+  }
   HADFL_KEEP(h, base, nullptr, messages);
   PackedWeights from;
   memset(&from, 0, sizeof(from));

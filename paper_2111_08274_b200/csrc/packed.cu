@@ -54,7 +54,9 @@ cudaError_t launch_dependent(void (*kernel)(Params...), unsigned grid, int threa
   early.val.programmaticStreamSerializationAllowed = 1;
   config.attrs = &early;
   config.numAttrs = 1;
-  return cudaLaunchKernelEx(&config, kernel, static_cast<Params>(args)...);
+  const cudaError_t rc = cudaLaunchKernelEx(&config, kernel, static_cast<Params>(args)...);
+  if (rc != cudaSuccess) cudaGetLastError();  // it is this call's, and not to be found by the next one
+  return rc;
 }
 
 bool at_32(const void *p) { return ((uintptr_t)p & 31u) == 0; }
@@ -157,8 +159,27 @@ cudaError_t launch_aggregate_packed(const PackedShape &s, const PackedWeights &w
   return rc;
 }
 
-size_t packed_dots_scratch_bytes(int sm_count) {
-  return sizeof(double) * (size_t)sm_count * kPackedMaxRows * kPackedMaxRows;
+namespace {
+
+// Rows of a message's pieces in a tile (a power of two), and blocks of a launch.
+int dots_rows(int most) {
+  int rows = 1;
+  while (rows < most) rows *= 2;
+  return rows;
+}
+int64_t dots_tiles(int64_t n_params, int rows) {
+  const int64_t pieces = (n_params + kDotsPiece - 1) / kDotsPiece;
+  const int segments = kDotsRows / rows;
+  return (pieces + segments - 1) / segments;
+}
+int dots_blocks(int64_t tiles, int sm_count) { return (int)(tiles < sm_count ? tiles : sm_count); }
+
+}  // namespace
+
+size_t packed_dots_scratch_bytes(int sm_count, int n_devices, int64_t n_params) {
+  // Fewer messages make tiles of more parameters, and not more blocks.
+  const int blocks = dots_blocks(dots_tiles(n_params, dots_rows(n_devices)), sm_count);
+  return sizeof(double) * (size_t)blocks * (size_t)n_devices * (size_t)n_devices;
 }
 
 cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
@@ -167,16 +188,13 @@ cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, c
   q.a = a_rows;
   q.b = b_rows;
   const bool same = a == b && a_rows.n == b_rows.n && memcmp(a_rows.id, b_rows.id, sizeof(a_rows.id)) == 0;
-  const int most = a_rows.n > b_rows.n ? a_rows.n : b_rows.n;
-  q.rows = 1;
-  while (q.rows < most) q.rows *= 2;
+  q.rows = dots_rows(a_rows.n > b_rows.n ? a_rows.n : b_rows.n);
   q.segments = kDotsRows / q.rows;
   q.blocks = (s.n_params + kPackedBlock - 1) / kPackedBlock;
   q.scales_at = packed_scales_at(s.n_params);
   q.message_bytes = packed_bytes(s.n_params);
-  const int64_t pieces = (s.n_params + kDotsPiece - 1) / kDotsPiece;
-  q.tiles = (pieces + q.segments - 1) / q.segments;
-  const int blocks = (int)(q.tiles < s.sm_count ? q.tiles : s.sm_count);
+  q.tiles = dots_tiles(s.n_params, q.rows);
+  const int blocks = dots_blocks(q.tiles, s.sm_count);
   const int pairs = a_rows.n * b_rows.n;
   double *partials = (double *)scratch;
   cudaError_t rc = cudaSuccess;

@@ -51,7 +51,7 @@ cudaError_t launch_aggregate_packed(const PackedShape &s, const PackedWeights &w
                              bool move_base, const uint8_t *messages);
 // out[i * b_rows.n + j] = sum over the parameters of message a_rows.id[i] of a times message b_rows.id[j] of b.
 // scratch: packed_dots_scratch_bytes() bytes.
-size_t packed_dots_scratch_bytes(int sm_count);
+size_t packed_dots_scratch_bytes(int sm_count, int n_devices, int64_t n_params);
 cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
                                const uint8_t *b, float *out, void *scratch);
 

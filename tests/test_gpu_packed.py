@@ -396,6 +396,24 @@ def test_products_with_a_message_that_has_a_lost_block(block):
     assert np.all(np.abs(got[np.ix_(rest, rest)] - want) <= DOTS_TOL * size)
 
 
+@pytest.mark.parametrize("low_a,low_b", [(225, 5), (3, 230), (127, 127), (200, 60), (90, 90)])
+def test_products_of_far_scales(low_a, low_b):
+    """Scales far from 1 whose products are not: 2^(a - 127) 2^(b - 127) with a + b near 254, or small throughout."""
+    rng = np.random.default_rng([low_a, low_b])
+    a, b = Side(3, 8200), Side(3, 8200)
+    d = []
+    for s, low in ((a, low_a), (b, low_b)):
+        raws = [ref.random_message(rng, 8200, low, low + 20) for _ in range(3)]
+        for i, raw in enumerate(raws):
+            s.set_message(i, raw)
+        d.append(np.stack([ref.values(*ref.from_bytes(raw, 8200), 8200) for raw in raws]))
+    out = torch.zeros((3, 3), device="cuda")
+    a.h.packed_dots(range(3), a.messages.data_ptr(), out.data_ptr(), b_ids=range(3), b_messages_ptr=b.messages.data_ptr())
+    a.check_guards()
+    want, size = dots_reference(*d)
+    assert np.all(np.abs(out.cpu().numpy() - want) <= DOTS_TOL * size)
+
+
 def test_products_do_not_read_other_devices_messages():
     """Messages of devices that are not asked for may hold anything (here: NaN blocks throughout)."""
     rng = np.random.default_rng(21)
@@ -450,6 +468,7 @@ def test_refusals():
            lambda: s.h.aggregate_packed([0], ok, dst_ids=[1, 1]), lambda: s.h.aggregate_packed([0], ok, dst_ids=[4]),
            lambda: s.h.aggregate_packed([0], ok, dst_ids=[]), lambda: s.h.aggregate_packed([0], ok, move_base=True),
            lambda: s.h.aggregate_packed([0], ok + 4), lambda: s.h.aggregate_packed([0], ok, base_ptr=s.w.data_ptr() + 32),
+           lambda: s.h.aggregate_packed([0], ok, base_ptr=s.w[2].data_ptr(), move_base=True),
            lambda: s.h.packed_dots([], ok, out.data_ptr()), lambda: s.h.packed_dots([4], ok, out.data_ptr()),
            lambda: s.h.packed_dots([0] * 5, ok, out.data_ptr()), lambda: s.h.packed_dots([0], ok, None),
            lambda: s.h.packed_dots([0], ok, host.data_ptr()), lambda: s.h.packed_dots([0], ok, out.data_ptr() + 2),
@@ -564,6 +583,10 @@ def test_long_rows():
     h.unpack([1], messages.data_ptr(), base_ptr=w[0].data_ptr())
     h.synchronize()
     h.debug_check()
+    assert [float(w[1, q]) - 3.0 for q in places] == reads
+    w[1].zero_()
+    h.aggregate_packed([1], messages.data_ptr(), base_ptr=w[0].data_ptr(), dst_ids=[1])
+    h.synchronize()
     assert [float(w[1, q]) - 3.0 for q in places] == reads
     assert float(out) == sum(v * v for v in reads)
     assert float(w[1, places[-1] - 1]) == 3.0 and int(w[1, :p].ne(3.0).sum()) == len(places)
