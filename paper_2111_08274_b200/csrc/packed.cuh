@@ -180,9 +180,21 @@ struct PackParams {
   RowRandom random[kPackedMaxRows];
 };
 
-// Quantisation.  A thread walks over the rows of its columns with the base in registers.
+// Quantisation.  A thread walks over the rows of its columns with the base in registers, and loads the next row while it
+// works on one (with a residual, whose loads are twice as many bytes, other blocks do for that: 92 us instead of 111 for 4 of
+// 11.2 M fp32 parameters with stochastic rounding, which then has room for more blocks).
+// Bound by HBM, except with stochastic rounding and no residual, where the generator's instructions bind (18 per
+// parameter against 8.5 with rounding to nearest).  Measured, us, and of the copy bandwidth (of what has to be read and
+// written): 4 of 11.2 M fp32, base, residual, stochastic 92 (100 %); 16 of 14.7 M bf16, base, nearest 105 (91 %), stochastic
+// 176 (54 %); 4 of 2^27 fp32 alone 345 (108 %).
+// Blocks per SM: bf16 without a residual takes 64 registers a thread, 4 blocks, unless it is told to do with fewer for 5
+// (109.5 / 104.6 us for the 16 above); stochastic rounding, or a residual, loses by that (176 / 193, 80 / 85).
+template <typename WT, bool kResidual, bool kStochastic>
+constexpr int pack_min_blocks() {
+  return sizeof(WT) == 2 && !kResidual && !kStochastic ? 5 : 1;
+}
 template <typename WT, bool kBase, bool kResidual, bool kStochastic, bool k32>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, pack_min_blocks<WT, kResidual, kStochastic>())
 k_pack(const WT *__restrict__ w, const WT *base, float *__restrict__ residual, uint8_t *__restrict__ messages,
        PhiloxKeys keys, const __grid_constant__ PackParams q) {
   constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, kLanes = kPackedBlock / E;
@@ -350,7 +362,8 @@ struct UnpackParams {
   int64_t row_at[kPackedMaxRows], message_at[kPackedMaxRows];
 };
 
-// w[i] = base + d_i for the listed devices.
+// w[i] = base + d_i for the listed devices.  Bound by HBM: 16 of 14.7 M bf16 98 us, 93 % of the copy bandwidth; 4 of 2^27 fp32
+// 368 us, 101 %.
 template <typename WT, bool kBase, bool k32>
 __global__ void __launch_bounds__(kThreads)
 k_unpack(WT *w, const WT *base, const uint8_t *__restrict__ messages, const __grid_constant__ UnpackParams q) {
@@ -397,7 +410,9 @@ struct AggregateParams {
   int64_t row_at[kPackedMaxRows], message_at[kPackedMaxRows];
 };
 
-// Eq. 5 from messages: acc = a_0 d_0, acc = fma(a_j, d_j, acc); base + acc to the receivers and, on request, the base.
+// Eq. 5 from messages: acc = a_0 d_0, acc = fma(a_j, d_j, acc); base + acc to the receivers and, on request, the base.  Bound by
+// HBM: 4 of 8 fp32 devices of 11.2 M parameters 42 us, 90 % of the copy bandwidth; 16 of 32 bf16 devices of 23.5 M 166 us,
+// 92 %; 4 of 16 fp32 devices of 2^25 to all 386 us, 98 %.
 template <typename WT, bool kBase, bool k32>
 __global__ void __launch_bounds__(kThreads)
 k_aggregate_packed(WT *w, WT *base, const uint8_t *__restrict__ messages, const __grid_constant__ AggregateParams q) {
@@ -614,6 +629,11 @@ __device__ __forceinline__ void barrier_commit(uint64_t *barrier) {
 
 // A ring of tiles in shared memory between the warps that copy and the threads that ask for the products, an accumulator
 // between each of those and the warps that add them up.  partials[pair][block]: 64-bit sums of the block's tiles.
+// Bound by HBM for long messages, else by the way from the first copy to the last sum (about 5 us with the finish).  Measured,
+// us, and of the copy bandwidth: 32 of 23.5 M parameters 66 (93 %; 75 to 80 in a long run, under the power limit), two sets
+// of 32 of 16.8 M 89 (98 %), 8 of 11.2 M 13.5 (54 %), 4 of 100,000 4.9.  One thread that asks for products instead of
+// two: 103, 102, 17.6 us for the first three (what each tile waits for then adds up to more than its copies take); three:
+// 66 to 75, no gain.
 template <bool kSame>
 __global__ void __launch_bounds__(kDotsThreads)
 k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, double *__restrict__ partials,
