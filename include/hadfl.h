@@ -453,8 +453,9 @@ int hadfl_predict_version(const double *series, int32_t n_obs, double alpha, dou
  * address ranges the handle registered.  An access outside them is skipped (loads read zeros) and
  * recorded; no kernel traps or asserts; and every call marked "synchronises" (and
  * hadfl_synchronize) then returns HADFL_ERR_STATE.  It stands in for a memory checker.  One GPU
- * per process; slower (a table lookup per access; hadfl_init, hadfl_destroy and
- * hadfl_stats_noalloc synchronise the device).  Results are identical to the normal build. */
+ * per process; slower (a table lookup per access; hadfl_init, hadfl_destroy, hadfl_stats_noalloc and the first
+ * call of hadfl_pack and its siblings with a buffer synchronise the device, so that such a call is to be made once
+ * before it is captured).  Results are identical to the normal build. */
 
 /* 1 in the debug build, 0 otherwise. */
 int hadfl_debug_build(void);

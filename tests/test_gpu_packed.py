@@ -22,21 +22,23 @@ def _gpu():
 class Side:
     """A handle over tensors of its own, with messages, a base and residuals."""
 
-    def __init__(self, n, p, storage="fp32", seed=77, stream=None, pad=0, weight_mode=0):
+    def __init__(self, n, p, storage="fp32", seed=77, stream=None, pad=0, weight_mode=0, shift=0):
+        """shift: elements by which arena, residuals and messages begin behind a multiple of 512 bytes."""
         self.n, self.p, self.seed = n, p, seed
         self.stride = -(-p // 32) * 32 + pad
         self.dtype = torch.bfloat16 if storage == "bf16" else torch.float32
         self.stream = stream or torch.cuda.current_stream()
         with torch.cuda.stream(self.stream):
-            self.w = torch.zeros((n, self.stride), dtype=self.dtype, device="cuda")
+            self.w = torch.zeros(n * self.stride + shift, dtype=self.dtype, device="cuda")[shift:].view(n, self.stride)
             self.m = torch.zeros((n, self.stride), dtype=torch.float32, device="cuda")
             self.h = binding.Hadfl(n, p, dtype=STORAGE[storage], seed=seed, w_ptr=self.w.data_ptr(),
                                    m_ptr=self.m.data_ptr(), row_stride_elems=self.stride, weight_mode=weight_mode,
                                    stream=self.stream.cuda_stream)
             self.bytes = binding.hadfl_packed_bytes(p)
             self.raw = torch.full((n * self.bytes + 2 * GUARD,), 0xA5, dtype=torch.uint8, device="cuda")
-            self.messages = self.raw[GUARD:-GUARD].view(n, self.bytes)
-            self.residual = torch.zeros((n, self.stride), dtype=torch.float32, device="cuda")
+            at = GUARD - 16 * (shift > 0)
+            self.messages = self.raw[at:at + n * self.bytes].view(n, self.bytes)
+            self.residual = torch.zeros(n * self.stride + 4 * (shift > 0), device="cuda")[4 * (shift > 0):].view(n, self.stride)
         self.stream.synchronize()
 
     def rows(self, values):
@@ -51,7 +53,8 @@ class Side:
     def check_guards(self):
         self.h.synchronize()
         self.h.debug_check()
-        assert torch.all(self.raw[:GUARD] == 0xA5) and torch.all(self.raw[-GUARD:] == 0xA5)
+        at = self.messages.data_ptr() - self.raw.data_ptr()
+        assert torch.all(self.raw[:at] == 0xA5) and torch.all(self.raw[at + self.n * self.bytes:] == 0xA5)
 
     def message(self, i):
         return self.messages[i].cpu().numpy()
@@ -288,6 +291,40 @@ def test_aggregate_packed_with_a_receivers_row_as_base():
     s.check_guards()
     for i, x in enumerate((w[0], want, w[2], want)):
         assert_same(s.w[i, :3001].cpu().numpy(), x, i)
+
+
+@pytest.mark.parametrize("storage", ["fp32", "bf16"])
+@pytest.mark.parametrize("p", [1, 40, 4099])
+def test_buffers_at_odd_multiples_of_16_bytes(p, storage):
+    """Arena, base, residuals and messages that begin 16 bytes behind a multiple of 32: whole calls, as above."""
+    rng = np.random.default_rng([p, 9])
+    shift = 8 if storage == "bf16" else 4
+    s = Side(3, p, storage, pad=8, shift=shift)
+    assert s.w.data_ptr() % 32 == 16 and s.residual.data_ptr() % 32 == 16 and s.messages.data_ptr() % 32 == 16
+    w = s.rows((1e-2 * rng.standard_normal((3, p))).astype(np.float32))
+    room = torch.zeros(p + shift, dtype=s.dtype, device="cuda")
+    room[shift:] = s.base((1e-2 * rng.standard_normal(p)).astype(np.float32))[0]
+    base_t = room[shift:]
+    base = base_t.float().cpu().numpy()
+    residual = (1e-3 * rng.standard_normal((3, p))).astype(np.float32)
+    s.residual[:, :p] = torch.from_numpy(residual)
+    s.h.pack([2, 0], s.messages.data_ptr(), base_ptr=base_t.data_ptr(), residual_ptr=s.residual.data_ptr(), rounding=1, round_=1)
+    s.check_guards()
+    check_pack(s, w, [2, 0], base, residual, 1, 1)
+    d = [ref.values(*ref.from_bytes(s.message(i), p), p) for i in (0, 2)]
+    s.h.unpack([0], s.messages.data_ptr(), base_ptr=base_t.data_ptr())
+    s.check_guards()
+    assert_same(s.w[0, :p].float().cpu().numpy(), to_storage(base + d[0].astype(np.float32), s.dtype))
+    s.h.aggregate_packed([0, 2], s.messages.data_ptr(), base_ptr=base_t.data_ptr(), dst_ids=[1, 2], move_base=True)
+    s.check_guards()
+    want = to_storage(aggregate_reference([np.float32(0.5)] * 2, d, base), s.dtype)
+    for got in (s.w[1, :p], s.w[2, :p], base_t):
+        assert_same(got.float().cpu().numpy(), want)
+    out = torch.zeros(5, device="cuda")[1:].view(2, 2)
+    s.h.packed_dots([0, 2], s.messages.data_ptr(), out.data_ptr())
+    s.check_guards()
+    want, size = dots_reference(np.stack(d), np.stack(d))
+    assert np.all(np.abs(out.cpu().numpy() - want) <= DOTS_TOL * size + 1e-30)
 
 
 # ---- products --------------------------------------------------------------------------------------------------------
