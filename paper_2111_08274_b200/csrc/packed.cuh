@@ -187,11 +187,14 @@ struct PackParams {
 // parameter against 8.5 with rounding to nearest).  Measured, us, and of the copy bandwidth (of what has to be read and
 // written): 4 of 11.2 M fp32, base, residual, stochastic 92 (100 %); 16 of 14.7 M bf16, base, nearest 105 (91 %), stochastic
 // 176 (54 %); 4 of 2^27 fp32 alone 345 (108 %).
-// Blocks per SM: bf16 without a residual takes 64 registers a thread, 4 blocks, unless it is told to do with fewer for 5
-// (109.5 / 104.6 us for the 16 above); stochastic rounding, or a residual, loses by that (176 / 193, 80 / 85).
+// Blocks per SM that the compiler is to leave registers for (0: it chooses, mostly few registers and many blocks).  Measured, us,
+// packed and read, the compiler's choice / this one: bf16 without a residual, to nearest, 5 blocks with 48 registers
+// instead of 64: 16 of 14.7 M 207 / 202; with a residual 4 blocks, whose loads then go out together: 8 of 2 M fp32 51.5 / 47.4, 8
+// of 8.4 M 181 / 180.  The others lose with fewer blocks (4 of 2^27 fp32 727; left to one block 780, to five 746).
 template <typename WT, bool kResidual, bool kStochastic>
 constexpr int pack_min_blocks() {
-  return sizeof(WT) == 2 && !kResidual && !kStochastic ? 5 : 1;
+  if (kResidual) return 4;
+  return sizeof(WT) == 2 && !kStochastic ? 5 : 0;
 }
 template <typename WT, bool kBase, bool kResidual, bool kStochastic, bool k32>
 __global__ void __launch_bounds__(kThreads, pack_min_blocks<WT, kResidual, kStochastic>())
