@@ -69,6 +69,7 @@ struct hadfl_handle {
   int last_launch_rounds = 0;        // rounds in the most recent launch of the fused round kernel
   int last_launch_pack = 0;          // columns per thread in that launch
   void *d_dots = nullptr;  // products of messages: the blocks' partial sums
+  bool dots_smem[2] = {};  // ... and whether their kernel is allowed the shared memory that it takes [one set of messages]
   // model backup that overlaps with later rounds: staging row + copy stream
   void *d_backup = nullptr;
   size_t backup_elem = 4;        // bytes per staged parameter: 2 where memory is too short to widen bf16 on the device
@@ -1276,7 +1277,7 @@ int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const vo
   if (debug_keep(out, out_bytes)) return HADFL_ERR_CUDA;
 #endif
   HADFL_CUDA(h, launch_packed_dots(packed_shape(h), packed_rows(a_ids, m), (const uint8_t *)a_messages,
-                                   packed_rows(b_ids, n), (const uint8_t *)b_messages, out, h->d_dots));
+                                   packed_rows(b_ids, n), (const uint8_t *)b_messages, out, h->d_dots, h->dots_smem));
   h->launches += 2;
   return HADFL_OK;
 }

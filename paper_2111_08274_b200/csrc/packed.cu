@@ -183,7 +183,7 @@ size_t packed_dots_scratch_bytes(int sm_count, int n_devices, int64_t n_params) 
 }
 
 cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
-                               const uint8_t *b, float *out, void *scratch) {
+                               const uint8_t *b, float *out, void *scratch, bool (&shared_allowed)[2]) {
   DotsParams q;
   q.a = a_rows;
   q.b = b_rows;
@@ -202,8 +202,13 @@ cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, c
     using Stages = DotsStages<is_same.value>;
     auto kernel = k_packed_dots<is_same.value>;
     const int bytes = 1024 + Stages::value * Stages::bytes;
-    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (rc == cudaSuccess) rc = launch_dependent(kernel, (unsigned)blocks, kDotsThreads, bytes, s.stream, a, b, partials, q);
+    bool &allowed = shared_allowed[is_same.value];
+    if (!allowed) rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    allowed = rc == cudaSuccess;
+    if (allowed)
+      rc = launch_dependent(kernel, (unsigned)blocks, kDotsThreads, bytes, s.stream, a, b, partials, q);
+    else
+      cudaGetLastError();
   });
   if (rc != cudaSuccess) return rc;
   return launch_dependent(k_packed_dots_finish, (unsigned)((pairs + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0,

@@ -50,10 +50,10 @@ cudaError_t launch_unpack(const PackedShape &s, const PackedRows &rows, const vo
 cudaError_t launch_aggregate_packed(const PackedShape &s, const PackedWeights &weights, const PackedRows &receivers, void *base,
                              bool move_base, const uint8_t *messages);
 // out[i * b_rows.n + j] = sum over the parameters of message a_rows.id[i] of a times message b_rows.id[j] of b.
-// scratch: packed_dots_scratch_bytes() bytes.
+// scratch: packed_dots_scratch_bytes() bytes.  shared_allowed: kept by the handle, false at first.
 size_t packed_dots_scratch_bytes(int sm_count, int n_devices, int64_t n_params);
 cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, const uint8_t *a, const PackedRows &b_rows,
-                               const uint8_t *b, float *out, void *scratch);
+                               const uint8_t *b, float *out, void *scratch, bool (&shared_allowed)[2]);
 
 // Debug build: this file's kernels have a range table of their own.
 int packed_debug_publish(const void *table, size_t bytes);

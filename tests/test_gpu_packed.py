@@ -576,6 +576,51 @@ def test_two_handles_on_two_streams_at_once():
     assert torch.equal(sides[0].residual, sides[1].residual)
 
 
+def test_calls_wait_for_other_streams_and_copies_before_them():
+    """The kernels may start under the one before them in their stream: what else the stream waits for - an event of
+    another stream, a copy, a kernel of another kind - has to be done before they read all the same."""
+    rng = np.random.default_rng(33)
+    p = 3_000_017
+    other, stream = torch.cuda.Stream(), torch.cuda.Stream()
+    s = Side(2, p, stream=stream)
+    sets = [[torch.from_numpy(ref.random_message(rng, p)).cuda() for _ in range(2)] for _ in range(2)]
+    want = [[ref.values(*ref.from_bytes(m.cpu().numpy(), p), p).astype(np.float32) for m in two] for two in sets]
+    busy = torch.randn(4096, 4096, device="cuda")
+    for i in range(2):
+        s.messages[i].copy_(sets[0][i])
+    s.h.unpack([0, 1], s.messages.data_ptr())
+    torch.cuda.synchronize()
+    for r in range(12):
+        now = sets[r % 2]
+        with torch.cuda.stream(stream):
+            s.h.unpack([0, 1], s.messages.data_ptr())            # the kernel before, with the messages of the last turn
+            if r % 3 == 0:                                       # the new ones from another stream, late
+                event = torch.cuda.Event()
+                event.record(stream)
+                with torch.cuda.stream(other):
+                    other.wait_event(event)
+                    for _ in range(4):
+                        busy = torch.tanh(busy @ busy)
+                    for i in range(2):
+                        s.messages[i].copy_(now[i])
+                    event = torch.cuda.Event()
+                    event.record(other)
+                stream.wait_event(event)
+            elif r % 3 == 1:                                     # by copies in the stream
+                for i in range(2):
+                    s.messages[i].copy_(now[i], non_blocking=True)
+            else:                                                # by kernels that are not the library's
+                busy = torch.tanh(busy @ busy)
+                for i in range(2):
+                    torch.bitwise_or(now[i], now[i], out=s.messages[i])
+            s.h.unpack([1, 0], s.messages.data_ptr())
+            got = s.w[:, :p].clone()
+        stream.synchronize()
+        for i in range(2):
+            assert np.array_equal(got[i].cpu().numpy(), want[r % 2][i]), (r, i)
+    s.check_guards()
+
+
 def test_residuals_carry_what_messages_leave_out():
     """A constant update sent many times: the sum of the messages stays within one scale of the sum of the updates."""
     rng = np.random.default_rng(32)
