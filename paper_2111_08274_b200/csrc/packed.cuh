@@ -186,7 +186,7 @@ struct PackParams {
 // Bound by HBM, except with stochastic rounding and no residual, where the generator's instructions bind (18 per
 // parameter against 8.5 with rounding to nearest).  Measured, us, and of the copy bandwidth (of what has to be read and
 // written): 4 of 11.2 M fp32, base, residual, stochastic 92 (100 %); 16 of 14.7 M bf16, base, nearest 105 (91 %), stochastic
-// 176 (54 %); 4 of 2^27 fp32 alone 345 (108 %).
+// 172 (56 %); 4 of 2^27 fp32 alone 345 (108 %).
 // Blocks per SM that the compiler is to leave registers for (0: it chooses, mostly few registers and many blocks).  Measured, us,
 // packed and read, the compiler's choice / this one: bf16 without a residual, to nearest, 5 blocks with 48 registers
 // instead of 64: 16 of 14.7 M 207 / 202; with a residual 4 blocks, whose loads then go out together: 8 of 2 M fp32 51.5 / 47.4, 8
@@ -276,7 +276,7 @@ k_pack(const WT *__restrict__ w, const WT *base, float *__restrict__ residual, u
           float t[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) t[k] = u[8 * i + k];
-          if (large) {
+          if (__any_sync(0xFFFFFFFFu, large)) {  // (a branch: as a condition of each product it is 3 us of 176)
 #pragma unroll
             for (int k = 0; k < 8; ++k) t[k] = __fmul_rn(t[k], down);
           }
