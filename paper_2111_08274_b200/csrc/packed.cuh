@@ -2,9 +2,10 @@
 //
 // A message of P parameters is ceil(P / 32) blocks of 32 codes (e2m1: sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; two per
 // byte, the even parameter in the low half) and one byte per block, the power-of-two scale 2^(byte - 127) (255: the block
-// reads as NaN, as one with a value that is not finite or nearly so does).  With u the fp32 values to send and A the largest |u| of a block, the scale is the smallest power of two,
-// 2^-127 or larger, with A <= 6 * scale: no value is cut off, so stochastic rounding is free of bias and the residual of
-// a block at most one scale.
+// reads as NaN, as one with a value that is not finite or nearly so does).  With u the fp32 values to send and A the
+// largest |u| of a block, the scale is the smallest power of two, 2^-127 or larger, with A <= 6 * scale: no value is cut
+// off, so stochastic rounding is free of bias, and what nearest rounding leaves out is at most one scale (stochastic
+// rounding: below two).
 //
 // All of it streams: a thread has 32 bytes of a row of parameters, 8 fp32 or 16 bf16 values, and four or two
 // threads a block of 32, so that a warp's codes are one or two lines of 128 bytes.
@@ -183,6 +184,7 @@ struct PackParams {
 // Quantisation.  A thread walks over the rows of its columns with the base in registers, and loads the next row while it
 // works on one (with a residual, whose loads are twice as many bytes, other blocks do for that: 92 us instead of 111 for 4 of
 // 11.2 M fp32 parameters with stochastic rounding, which then has room for more blocks).
+//
 // Bound by HBM, except with stochastic rounding and no residual, where the generator's instructions bind (18 per
 // parameter against 8.5 with rounding to nearest).  Measured, us, and of the copy bandwidth (of what has to be read and
 // written): 4 of 11.2 M fp32, base, residual, stochastic 92 (100 %); 16 of 14.7 M bf16, base, nearest 105 (91 %), stochastic
@@ -490,10 +492,8 @@ constexpr uint32_t kDotsWaitNs = 1000, kDotsMaxWaits = 1u << 20;  // a wait ends
 
 struct DotsParams {
   PackedRows a, b;
-  int same;               // B is A: one tile, and only pairs i <= j
   int rows;               // R
-  int segments;           // pieces of a tile, at most 128 / R
-
+  int segments;           // pieces of a tile, 128 / R
   int64_t tiles;
   int64_t blocks;         // blocks of 32 parameters
   int64_t scales_at, message_bytes;
@@ -645,7 +645,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   constexpr int kStages = Stages::value;
   extern __shared__ uint8_t shared[];
   __shared__ __align__(8) uint64_t full[kStages], empty[kStages];
-  __shared__ __align__(8) uint64_t sum_full[kDotsMmaWarps], sum_empty[kDotsMmaWarps];
+  __shared__ __align__(8) uint64_t sum_full[kDotsMmaWarps], sum_empty[kDotsMmaWarps], drained[kDotsMmaWarps];
   __shared__ uint32_t tmem_base;
   __shared__ int failed;
   const uint32_t stages_at = (shared_address(shared) + 1023u) & ~1023u;
@@ -667,6 +667,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
     for (int i = 0; i < kDotsMmaWarps; ++i) {
       barrier_init(&sum_full[i], 1);
       barrier_init(&sum_empty[i], kDotsSumWarps);
+      barrier_init(&drained[i], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -687,7 +688,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base;
-  let_next_start();  // with the tensor memory allocated: a block of the next call waits for it without a place on this SM
+  let_next_start();  // all blocks have their tensor memory by then, so that those of the next call cannot be in their way
   double sum[32];
 
   if (warp < kDotsLoadWarps) {
@@ -764,6 +765,9 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
         ++f;
       }
     }
+    // Nothing is in flight when the tensor memory is given back, even if some wait above ran out.
+    barrier_commit(&drained[m]);
+    if (!barrier_wait(&drained[m], 0)) failed = 1;
   }
   __syncthreads();
   wait_for_stream();  // (done long since) what follows writes where the call before may have read
