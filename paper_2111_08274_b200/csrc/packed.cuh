@@ -481,11 +481,15 @@ constexpr int kDotsFlush = 64;      // 2^14 parameters per row
 constexpr int kDotsCodeBytes = kDotsRows * kDotsPiece / 2;
 constexpr int kDotsScaleBytes = kDotsRows * kDotsPiece / kPackedBlock;
 constexpr int kDotsSetBytes = kDotsCodeBytes + kDotsScaleBytes;
-constexpr int kDotsTmemColumns = 512;  // the accumulators, 128 each, and the scales of the tiles, up to 80
-// Tiles in shared memory.
+constexpr int kDotsTmemColumns = 512;  // the accumulators, 128 each, and the scales of the tiles, 64
+// Tiles in shared memory: a multiple of kDotsMmaWarps, so that a stage's tiles are asked for by one thread, one after the
+// other, and the parity of a phase tells which one is there.  Measured, us: one set of 32 messages of 23.5 M parameters with 4 /
+// 6 / 8 stages 78 / 67 / 65; two sets of 32 of 16.8 M with 4 / 6 89 / 134 (six leave the L1 18 KB, and the scales' copies of
+// 4 bytes share their sectors there).
 template <bool kSame>
 struct DotsStages {
-  static constexpr int value = kSame ? 8 : 5;
+  static constexpr int value = kSame ? 8 : 4;
+  static_assert(value % kDotsMmaWarps == 0);
   static constexpr int bytes = (kSame ? 1 : 2) * kDotsSetBytes;
 };
 constexpr uint32_t kDotsWaitNs = 1000, kDotsMaxWaits = 1u << 20;  // a wait ends after a second or so
@@ -635,7 +639,7 @@ __device__ __forceinline__ void barrier_commit(uint64_t *barrier) {
 // Bound by HBM for long messages, else by the way from the first copy to the last sum (about 5 us with the finish).  Measured,
 // us, and of the copy bandwidth: 32 of 23.5 M parameters 66 (93 %; 75 to 80 in a long run, under the power limit), two sets
 // of 32 of 16.8 M 89 (98 %), 8 of 11.2 M 13.5 (54 %), 4 of 100,000 4.9.  One thread that asks for products instead of
-// two: 103, 102, 17.6 us for the first three (what each tile waits for then adds up to more than its copies take); three:
+// two: 103, 102, 17.6 us for these three (what each tile waits for then adds up to more than its copies take); three:
 // 66 to 75, no gain.
 template <bool kSame>
 __global__ void __launch_bounds__(kDotsThreads)
