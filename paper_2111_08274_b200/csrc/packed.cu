@@ -161,15 +161,10 @@ cudaError_t launch_aggregate_packed(const PackedShape &s, const PackedWeights &w
 
 namespace {
 
-// Rows of a message's pieces in a tile (a power of two), and blocks of a launch.
-int dots_rows(int most) {
-  int rows = 1;
-  while (rows < most) rows *= 2;
-  return rows;
-}
+// Tiles of a launch, with `rows` the larger number of messages, and its blocks.
 int64_t dots_tiles(int64_t n_params, int rows) {
   const int64_t pieces = (n_params + kDotsPiece - 1) / kDotsPiece;
-  const int segments = kDotsRows / rows;
+  const int segments = kDotsRows / 32 * (32 / rows);
   return (pieces + segments - 1) / segments;
 }
 int dots_blocks(int64_t tiles, int sm_count) { return (int)(tiles < sm_count ? tiles : sm_count); }
@@ -178,7 +173,7 @@ int dots_blocks(int64_t tiles, int sm_count) { return (int)(tiles < sm_count ? t
 
 size_t packed_dots_scratch_bytes(int sm_count, int n_devices, int64_t n_params) {
   // Fewer messages make tiles of more parameters, and not more blocks.
-  const int blocks = dots_blocks(dots_tiles(n_params, dots_rows(n_devices)), sm_count);
+  const int blocks = dots_blocks(dots_tiles(n_params, n_devices), sm_count);
   return sizeof(double) * (size_t)blocks * (size_t)n_devices * (size_t)n_devices;
 }
 
@@ -188,8 +183,9 @@ cudaError_t launch_packed_dots(const PackedShape &s, const PackedRows &a_rows, c
   q.a = a_rows;
   q.b = b_rows;
   const bool same = a == b && a_rows.n == b_rows.n && memcmp(a_rows.id, b_rows.id, sizeof(a_rows.id)) == 0;
-  q.rows = dots_rows(a_rows.n > b_rows.n ? a_rows.n : b_rows.n);
-  q.segments = kDotsRows / q.rows;
+  q.rows = a_rows.n > b_rows.n ? a_rows.n : b_rows.n;
+  q.per_warp = 32 / q.rows;
+  q.segments = kDotsRows / 32 * q.per_warp;
   q.blocks = (s.n_params + kPackedBlock - 1) / kPackedBlock;
   q.scales_at = packed_scales_at(s.n_params);
   q.message_bytes = packed_bytes(s.n_params);

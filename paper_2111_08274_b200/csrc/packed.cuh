@@ -464,9 +464,12 @@ k_aggregate_packed(WT *w, WT *base, const uint8_t *__restrict__ messages, const 
 // Products of messages, out = A B^T over the parameters, on the tensor cores: the codes and scales of a message are what
 // tcgen05.mma kind::mxf4 takes (e2m1 with one ue8m0 scale per 32 along K), so they go from HBM to shared memory as they
 // are and are never decoded.  A and B have up to 32 rows, the instruction 128 of each.  The K axis fills them: with R the
-// rows rounded up to a power of two, row s R + i of a tile is message i at the s-th of 128 / R consecutive pieces of
-// 256 parameters, in A and in B.  The accumulator's R x R blocks on the diagonal are then sums over 128 / R pieces at
-// once, and the rest of it is not read.  (With the messages in rows 0 .. R-1 alone every instruction would read 128 rows
+// larger number of rows and g = floor(32 / R), each 32 rows of a tile are all messages at g of 4 g consecutive pieces of
+// 256 parameters, one after the other, in A and in B.  The accumulator's R x R blocks on the diagonal are then sums over
+// as many pieces at once, each within the 32 x 32 of one warp's lanes, and the rest of it is not read.  (R rounded up to a
+// power of two instead, with 128 / R pieces: 5 messages of 26.8 M parameters 19.9 us, against 15.4.  Blocks that go on
+// across the bounds of the 32 rows, 128 / R of them whatever R: the scales of a piece then no longer begin at a sector, and
+// sums cannot stay in registers: 17 messages of 7.9 M 23.3 us, against 21.4.)  (With the messages in rows 0 .. R-1 alone every instruction would read 128 rows
 // of shared memory for R rows of data, which at R = 8 takes five times as long as HBM takes to deliver them.)
 // Rows that no message fills hold whatever was there: a row of A or B reaches its own row or column of the product only.
 // The accumulator is fp32 in TMEM, where a long sum of one sign loses bits, so that every kDotsFlush tiles it is added
@@ -497,7 +500,8 @@ constexpr uint32_t kDotsWaitNs = 1000, kDotsMaxWaits = 1u << 20;  // a wait ends
 struct DotsParams {
   PackedRows a, b;
   int rows;               // R
-  int segments;           // pieces of a tile, 128 / R
+  int per_warp;           // pieces that 32 rows hold, g
+  int segments;           // pieces of a tile, 4 g
   int64_t tiles;
   int64_t blocks;         // blocks of 32 parameters
   int64_t scales_at, message_bytes;
@@ -571,6 +575,15 @@ __device__ __forceinline__ void tmem_load_32(uint32_t at, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// What row r of a tile holds: a message and one of the tile's pieces, -1 where it holds none.
+struct DotsRow {
+  int message, segment;
+};
+__device__ __forceinline__ DotsRow dots_row(int r, const DotsParams &q) {
+  const int s = (r & 31) / q.rows;
+  return DotsRow{(r & 31) - s * q.rows, s < q.per_warp ? (r >> 5) * q.per_warp + s : -1};
+}
+
 // One thread's part of a tile's copies: four pieces of 16 bytes of codes, and four scales.
 struct DotsLoader {
   static constexpr int kThreadsOf = 32 * kDotsLoadWarps, kPieces = kDotsRows * 8 / kThreadsOf;
@@ -578,25 +591,25 @@ struct DotsLoader {
   int64_t block[kPieces], scale_block;     // and which block of 32 parameters that is
   uint32_t to[kPieces], scales_to;         // places in a set
 
-  __device__ __forceinline__ void start(const uint8_t *messages, const PackedRows &ids, const DotsParams &q, int log_rows) {
-    auto message = [&](int r) -> const uint8_t * {
-      const int i = r & (q.rows - 1);
-      return i < ids.n && r >> log_rows < q.segments ? messages + ids.id[i] * q.message_bytes : nullptr;
-    };
+  __device__ __forceinline__ void start(const uint8_t *messages, const PackedRows &ids, const DotsParams &q) {
     const int c = threadIdx.x & 7;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int r = i * (kThreadsOf / 8) + (threadIdx.x >> 3);
-      const uint8_t *m = message(r);
-      block[i] = (int64_t)(r >> log_rows) * 8 + c;
-      codes[i] = m ? m + block[i] * 16 : nullptr;
+      const DotsRow row = dots_row(r, q);
+      block[i] = (int64_t)row.segment * 8 + c;
+      codes[i] = start_of(messages, row, ids, q, block[i] * 16);
       to[i] = r * 128 + ((c ^ (r & 7)) << 4);  // 16-byte pieces change places within a row, the 128-byte swizzle
     }
     const int r = threadIdx.x & (kDotsRows - 1), g = threadIdx.x / kDotsRows;
-    const uint8_t *m = message(r);
-    scale_block = (int64_t)(r >> log_rows) * 8 + 4 * g;
-    scales = m ? m + q.scales_at + scale_block : nullptr;
+    const DotsRow row = dots_row(r, q);
+    scale_block = (int64_t)row.segment * 8 + 4 * g;
+    scales = start_of(messages, row, ids, q, q.scales_at + scale_block);
     scales_to = kDotsCodeBytes + g * 512 + (r & 31) * 16 + (r >> 5) * 4;
+  }
+  static __device__ __forceinline__ const uint8_t *start_of(const uint8_t *messages, const DotsRow &row,
+                                                            const PackedRows &ids, const DotsParams &q, int64_t offset) {
+    return row.segment >= 0 && row.message < ids.n ? messages + ids.id[row.message] * q.message_bytes + offset : nullptr;
   }
   // at: the set's place in a stage.  What lies behind the last block is filled with zeros.
   __device__ __forceinline__ void load(uint32_t at, int64_t tile, const DotsParams &q) const {
@@ -636,9 +649,10 @@ __device__ __forceinline__ void barrier_commit(uint64_t *barrier) {
 
 // A ring of tiles in shared memory between the warps that copy and the threads that ask for the products, an accumulator
 // between each of those and the warps that add them up.  partials[pair][block]: 64-bit sums of the block's tiles.
-// Bound by HBM for long messages, else by the way from the first copy to the last sum (about 5 us with the finish).  Measured,
-// us, and of the copy bandwidth: 32 of 23.5 M parameters 66 (93 %; 75 to 80 in a long run, under the power limit), two sets
-// of 32 of 16.8 M 89 (98 %), 8 of 11.2 M 13.5 (54 %), 4 of 100,000 4.9.  One thread that asks for products instead of
+// Bound by HBM for long messages, else by the way from the first copy to the last sum (about 4 us with the finish).  Measured,
+// us, and of the copy bandwidth: 32 of 23.5 M parameters 65 (94 %; 75 to 80 in a long run, under the power limit), two sets
+// of 32 of 16.8 M 89 (98 %), 8 of 11.2 M 12.3 (59 %), 4 of 100,000 3.9; of 2^27 parameters in all, 5 messages 15.4 (71 %), 9
+// 15.9, and 17, which leave the lower half of every 32 rows empty, 21.4 (51 %).  One thread that asks for products instead of
 // two: 103, 102, 17.6 us for these three (what each tile waits for then adds up to more than its copies take); three:
 // 66 to 75, no gain.
 template <bool kSame>
@@ -654,7 +668,6 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   __shared__ int failed;
   const uint32_t stages_at = (shared_address(shared) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int log_rows = 31 - __clz(q.rows);
   const int n_tiles = (int)((q.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x);
   if (warp == kDotsLoadWarps) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&tmem_base)),
@@ -683,8 +696,8 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
     if (!kSame) from_b.load(to + kDotsSetBytes, tile, q);
   };
   if (warp < kDotsLoadWarps) {
-    from_a.start(a, q.a, q, log_rows);
-    if (!kSame) from_b.start(b, q.b, q, log_rows);
+    from_a.start(a, q.a, q);
+    if (!kSame) from_b.start(b, q.b, q);
     wait_for_stream();
     load(0);
   }
@@ -710,7 +723,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   } else if (warp < kDotsLoadWarps + kDotsSumWarps) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) sum[i] = 0.0;
-    // Row r needs columns r / R * R .. + R - 1: they lie among the 32 of its warp's rows.
+    // What a row needs of the accumulator lies among the columns with its warp's 32 rows' numbers.
     const uint32_t rows = (warp - kDotsLoadWarps) * 32;
     const int n_sums = (n_tiles + kDotsMmaWarps * kDotsFlush - 1) / (kDotsMmaWarps * kDotsFlush);
     for (int f = 0; f < n_sums; ++f) {
@@ -778,21 +791,25 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   // The blocks on the diagonal, [segment][j][i], in the stages' place (whose last products are in the sums).
   double *mine = reinterpret_cast<double *>(shared + (stages_at - shared_address(shared)));
   if (warp >= kDotsLoadWarps && warp < kDotsLoadWarps + kDotsSumWarps) {
-    const int r = threadIdx.x - 32 * kDotsLoadWarps, i = r & (q.rows - 1), s = r >> log_rows;
+    const DotsRow row = dots_row(threadIdx.x - 32 * kDotsLoadWarps, q);
+    const int begin = lane - row.message;  // of the row's block among the warp's columns
 #pragma unroll
-    for (int c = 0; c < 32; ++c)
-      if ((c >> log_rows) == (lane >> log_rows)) mine[(((s << log_rows) + (c & (q.rows - 1))) << log_rows) + i] = sum[c];
+    for (int c = 0; c < 32; ++c) {
+      const int j = c - begin;
+      if (row.segment >= 0 && j >= 0 && j < q.rows) mine[(row.segment * q.rows + j) * q.rows + row.message] = sum[c];
+    }
   }
   __syncthreads();
-  // A lane has every `lanes`-th segment of a pair, four of them; then a butterfly over a pair's lanes.
-  const int log_lanes = min(5, 5 - log_rows), per_warp = 32 >> log_lanes, part = lane >> (5 - log_lanes);
-  const int all = q.rows << log_rows;
+  // A lane has every `lanes`-th segment of a pair, four to six of them; then a butterfly over a pair's lanes.
+  const int log_lanes = 31 - __clz(q.per_warp), per_warp = 32 >> log_lanes, part = lane >> (5 - log_lanes);
+  const int all = q.rows * q.rows;
   for (int e0 = warp * per_warp; e0 < all; e0 += kDotsThreads / 32 * per_warp) {
-    const int e = e0 + (lane & (per_warp - 1)), i = e & (q.rows - 1), j = e >> log_rows;
+    const int e = e0 + (lane & (per_warp - 1)), j = e / q.rows, i = e - j * q.rows;
     double total = 0.0;
-    for (int s = part; s < q.segments; s += 1 << log_lanes) total += mine[(s << (2 * log_rows)) + e];
+    if (e < all)
+      for (int s = part; s < q.segments; s += 1 << log_lanes) total += mine[s * all + e];
     for (int off = 16; off >= per_warp; off >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, off);
-    if (part || i >= q.a.n || j >= q.b.n || (kSame && i > j)) continue;
+    if (part || e >= all || i >= q.a.n || j >= q.b.n || (kSame && i > j)) continue;
     // A wait that ran out (which nothing is known to cause) shows as products that are no numbers.
     double *at = partials + (int64_t)(i * q.b.n + j) * gridDim.x + blockIdx.x;
     if (access_ok(at, 8)) *at = failed ? __longlong_as_double(0x7FF8000000000000ll) : total;
