@@ -342,7 +342,7 @@ def dots_reference(x, y):
 
 
 @pytest.mark.parametrize("p", SIZES + [70_001])
-@pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 9, 17, 32])
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 6, 7, 8, 9, 10, 11, 16, 17, 31, 32])
 def test_products_of_one_set(p, n):
     rng = np.random.default_rng([p, n])
     s = Side(n, p)
@@ -360,7 +360,7 @@ def test_products_of_one_set(p, n):
     assert np.array_equal(got, got.T)
 
 
-@pytest.mark.parametrize("m,n", [(1, 32), (32, 1), (3, 7), (2, 2), (16, 5), (5, 17)])
+@pytest.mark.parametrize("m,n", [(1, 32), (32, 1), (3, 7), (2, 2), (16, 5), (5, 17), (10, 3), (6, 6)])
 @pytest.mark.parametrize("p", [1, 95, 4096, 66_007])
 def test_products_of_two_sets(p, m, n):
     rng = np.random.default_rng([p, m, n])
