@@ -65,11 +65,12 @@ bool at_32(const void *p) { return ((uintptr_t)p & 31u) == 0; }
 // fewer where the columns alone make less than two blocks per SM.  Measured, us, all rows / split: pack, 2 of 100,000 fp32
 // parameters (25 or 49 blocks of columns) 2.40 / 1.96; 32 of 200,000 fp32 (98 blocks) 11.8 / 6.6; 16 of 300,000 bf16 (74)
 // 6.3 / 5.7; from two blocks per SM on no split: 16 of 1 M fp32 (489) 33.1 / 37.1.
+// together: no split, where one block may not write what another one reads.
 template <typename Params>
-unsigned split_rows(const PackedShape &s, const PackedRows &rows, int64_t columns, Params &q) {
+unsigned split_rows(const PackedShape &s, const PackedRows &rows, int64_t columns, bool together, Params &q) {
   const unsigned blocks = column_blocks(s.bf16, columns);
   const unsigned sms = (unsigned)s.sm_count;
-  const int split = blocks < 2 * sms ? (int)((4 * sms + blocks - 1) / blocks) : 1;
+  const int split = blocks < 2 * sms && !together ? (int)((4 * sms + blocks - 1) / blocks) : 1;
   q.n = rows.n;
   q.rows_per_block = split < rows.n ? (rows.n + split - 1) / split : 1;
   q.row_blocks = (rows.n + q.rows_per_block - 1) / q.rows_per_block;
@@ -90,7 +91,7 @@ cudaError_t launch_pack(const PackedShape &s, const PackedRows &rows, const void
   const int64_t scales_at = packed_scales_at(s.n_params);
   q.code_columns = scales_at * 2;
   q.scale_columns = (packed_bytes(s.n_params) - scales_at) * kPackedBlock;
-  const unsigned grid = split_rows(s, rows, q.scale_columns, q);
+  const unsigned grid = split_rows(s, rows, q.scale_columns, false, q);
   q.tag = kTagPack | ((uint32_t)(round >> 32) & 0xFFFFFFu);
   for (int j = 0; j < rows.n; ++j) {
     // The rounds of the generator that the device takes part in alone (see random_words).
@@ -118,7 +119,11 @@ cudaError_t launch_pack(const PackedShape &s, const PackedRows &rows, const void
 
 cudaError_t launch_unpack(const PackedShape &s, const PackedRows &rows, const void *base, const uint8_t *messages) {
   UnpackParams q;
-  const unsigned grid = split_rows(s, rows, s.n_params, q);
+  // A base that is one of the rows to be written: a thread loads it before it writes any row of its columns.
+  bool base_is_written = false;
+  for (int j = 0; j < rows.n; ++j)
+    base_is_written |= base == (const char *)s.w + rows.id[j] * s.stride * (s.bf16 ? 2 : 4);
+  const unsigned grid = split_rows(s, rows, s.n_params, base_is_written, q);
   cudaError_t rc = cudaSuccess;
   with_storage(s.bf16, [&](auto wt) {
     using WT = typename decltype(wt)::type;

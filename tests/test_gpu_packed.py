@@ -232,6 +232,25 @@ def test_unpack(p, storage, base_is):
         assert np.array_equal(s.message(i), raws[i])
 
 
+@pytest.mark.parametrize("storage", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,p,which", [(32, 100_003, 0), (32, 20_000, 31), (9, 300_001, 4), (32, 1_000_003, 16)])
+def test_unpack_with_a_base_that_is_written_too(n, p, which, storage):
+    """All rows are base + message with the base as it was before the call, the base's own row among them."""
+    rng = np.random.default_rng([n, p])
+    s = Side(n, p, storage)
+    raws = [ref.random_message(rng, p) for _ in range(n)]
+    d = [ref.values(*ref.from_bytes(raw, p), p).astype(np.float32) for raw in raws]
+    for i in range(n):
+        s.set_message(i, raws[i])
+    for turn in range(4):
+        w = s.rows(rng.standard_normal((n, p), dtype=np.float32))
+        s.h.unpack(rng.permutation(n), s.messages.data_ptr(), base_ptr=s.w[which].data_ptr())
+        s.check_guards()
+        got = s.w[:, :p].float().cpu().numpy()
+        for i in range(n):
+            assert_same(got[i], to_storage(w[which] + d[i], s.dtype), (turn, i))
+
+
 def fused_multiply_add(a, d, c):
     """fl(a * d + c), rounded to fp32 once.  The product is exact in the 64 bits of a long double; where the sum is not,
     it is moved by one of its own last places towards what it left out, so that no tie of fp32 is made of it."""
