@@ -560,8 +560,22 @@ __device__ __forceinline__ void dots_mma(uint32_t tmem, uint64_t a, uint64_t b, 
       : "memory");
 }
 
+// Tensor memory.  These instructions are aligned, that is undefined where the lanes of a warp are apart (behind a wait, a
+// loop or a branch that each lane takes by itself), so that the lanes meet before each; all of them come here or none.
+__device__ __forceinline__ void tmem_alloc(uint32_t *base) {
+  __syncwarp();
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(base)),
+               "n"(kDotsTmemColumns)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t base) {
+  __syncwarp();
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "n"(kDotsTmemColumns) : "memory");
+}
 __device__ __forceinline__ void tmem_load_32(uint32_t at, float (&v)[32]) {
   uint32_t r[32];
+  __syncwarp();
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
       "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -669,12 +683,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
   const uint32_t stages_at = (shared_address(shared) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n_tiles = (int)((q.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x);
-  if (warp == kDotsLoadWarps) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&tmem_base)),
-                 "n"(kDotsTmemColumns)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == kDotsLoadWarps) tmem_alloc(&tmem_base);
   if (warp == kDotsLoadWarps + 1 && lane == 0) {
     failed = 0;
     for (int i = 0; i < kStages; ++i) {
@@ -726,10 +735,16 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
     // What a row needs of the accumulator lies among the columns with its warp's 32 rows' numbers.
     const uint32_t rows = (warp - kDotsLoadWarps) * 32;
     const int n_sums = (n_tiles + kDotsMmaWarps * kDotsFlush - 1) / (kDotsMmaWarps * kDotsFlush);
-    for (int f = 0; f < n_sums; ++f) {
+    bool there = true;
+    for (int f = 0; f < n_sums && there; ++f) {
       for (int m = 0; m < kDotsMmaWarps; ++m) {
         if (n_tiles <= m + f * kDotsMmaWarps * kDotsFlush) break;
-        if (!barrier_wait(&sum_full[m], f & 1)) failed = 1;
+        // One answer for the warp: its lanes go on, or stop, together.
+        there = __all_sync(0xFFFFFFFFu, barrier_wait(&sum_full[m], f & 1));
+        if (!there) {
+          failed = 1;
+          break;
+        }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         float v[32];
         tmem_load_32(tmem + (rows << 16) + m * kDotsRows + rows, v);
@@ -739,7 +754,6 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
 #pragma unroll
         for (int i = 0; i < 32; ++i) sum[i] += (double)v[i];
       }
-      if (failed) break;
     }
   } else if (lane == 0) {
     // Warp m takes the tiles t = m, m + kDotsMmaWarps, ...: what one tile has to wait for (its copies, the fence, its
@@ -814,8 +828,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
     double *at = partials + (int64_t)(i * q.b.n + j) * gridDim.x + blockIdx.x;
     if (access_ok(at, 8)) *at = failed ? __longlong_as_double(0x7FF8000000000000ll) : total;
   }
-  if (warp == kDotsLoadWarps)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kDotsTmemColumns) : "memory");
+  if (warp == kDotsLoadWarps) tmem_free(tmem);
 }
 
 // out[pair] = sum of the blocks' partial sums in a fixed order, a warp per pair; of a set with itself each sum is for two.

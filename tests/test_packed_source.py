@@ -1,0 +1,24 @@
+"""What has to hold of the messages' kernels by their source, where a fault would be a hang or a race on the GPU that no
+run is sure to show (csrc/packed.cuh is read as text)."""
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def source():
+    text = open(os.path.join(ROOT, "paper_2111_08274_b200", "csrc", "packed.cuh")).read()
+    return re.sub(r"//[^\n]*", "", text)
+
+
+def test_lanes_are_together_before_aligned_instructions_on_tensor_memory(source):
+    """tcgen05.alloc, .ld and .dealloc are undefined (they may hang) when a warp's lanes are apart, as they may be behind a
+    wait, a loop or a branch of each lane: a __syncwarp() comes directly before."""
+    found = [m for m in re.finditer(r'asm volatile\(\s*"tcgen05\.(alloc|ld|dealloc)\b', source)]
+    assert sorted(m[1] for m in found) == ["alloc", "dealloc", "ld"]
+    assert len(found) == len(re.findall(r"tcgen05\.(?:alloc|ld|dealloc)\b", source))
+    for m in found:
+        assert source[:m.start()].rstrip().endswith("__syncwarp();"), m[1]
