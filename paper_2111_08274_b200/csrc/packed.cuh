@@ -22,7 +22,10 @@ constexpr uint32_t kPackedNan = 255;
 
 // The kernels here are launched as dependents of what is before them in the stream (launch_dependent): their blocks may
 // become resident while the kernel before still runs, and touch no memory before this.  It returns when that kernel is
-// done and its writes are visible; as every kernel here begins with it, so is everything before that.
+// done and its writes are visible; as every kernel here begins with it, so is everything before that.  Data that the kernel
+// before may write are read by ordinary loads (or cp.async) behind the wait: no kernel here has a __restrict__ pointer, which
+// would promise that nobody writes the data while the kernel is there, and so allow loads through the read-only path or
+// ahead of the wait.
 __device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // The kernel behind this one may become resident once all blocks are here.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -200,7 +203,7 @@ constexpr int pack_min_blocks() {
 }
 template <typename WT, bool kBase, bool kResidual, bool kStochastic, bool k32>
 __global__ void __launch_bounds__(kThreads, pack_min_blocks<WT, kResidual, kStochastic>())
-k_pack(const WT *__restrict__ w, const WT *base, float *__restrict__ residual, uint8_t *__restrict__ messages,
+k_pack(const WT *w, const WT *base, float *residual, uint8_t *messages,
        PhiloxKeys keys, const __grid_constant__ PackParams q) {
   constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, kLanes = kPackedBlock / E;
   constexpr bool kPrefetch = !kResidual;
@@ -371,7 +374,7 @@ struct UnpackParams {
 // 368 us, 101 %.
 template <typename WT, bool kBase, bool k32>
 __global__ void __launch_bounds__(kThreads)
-k_unpack(WT *w, const WT *base, const uint8_t *__restrict__ messages, const __grid_constant__ UnpackParams q) {
+k_unpack(WT *w, const WT *base, const uint8_t *messages, const __grid_constant__ UnpackParams q) {
   constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, B = kPackedBatch;
   const int64_t block = blockIdx.x / q.row_blocks;
   const int64_t column = E * (block * kThreads + threadIdx.x);
@@ -420,7 +423,7 @@ struct AggregateParams {
 // 92 %; 4 of 16 fp32 devices of 2^25 to all 386 us, 98 %.
 template <typename WT, bool kBase, bool k32>
 __global__ void __launch_bounds__(kThreads)
-k_aggregate_packed(WT *w, WT *base, const uint8_t *__restrict__ messages, const __grid_constant__ AggregateParams q) {
+k_aggregate_packed(WT *w, WT *base, const uint8_t *messages, const __grid_constant__ AggregateParams q) {
   constexpr int E = PackedE<WT>::value, kParts = PackedE<WT>::parts, B = kPackedBatch;
   const int64_t block = blockIdx.x;
   const int64_t column = E * (block * kThreads + threadIdx.x);
@@ -671,7 +674,7 @@ __device__ __forceinline__ void barrier_commit(uint64_t *barrier) {
 // 66 to 75, no gain.
 template <bool kSame>
 __global__ void __launch_bounds__(kDotsThreads)
-k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, double *__restrict__ partials,
+k_packed_dots(const uint8_t *a, const uint8_t *b, double *partials,
               const __grid_constant__ DotsParams q) {
   using Stages = DotsStages<kSame>;
   constexpr int kStages = Stages::value;
@@ -833,7 +836,7 @@ k_packed_dots(const uint8_t *__restrict__ a, const uint8_t *__restrict__ b, doub
 
 // out[pair] = sum of the blocks' partial sums in a fixed order, a warp per pair; of a set with itself each sum is for two.
 __global__ void __launch_bounds__(kThreads)
-k_packed_dots_finish(const double *__restrict__ partials, int n_blocks, int m, int n, int same, float *__restrict__ out) {
+k_packed_dots_finish(const double *partials, int n_blocks, int m, int n, int same, float *out) {
   const int p = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int i = p / n, j = p - i * n;
   let_next_start();

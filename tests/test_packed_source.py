@@ -22,3 +22,13 @@ def test_lanes_are_together_before_aligned_instructions_on_tensor_memory(source)
     assert len(found) == len(re.findall(r"tcgen05\.(?:alloc|ld|dealloc)\b", source))
     for m in found:
         assert source[:m.start()].rstrip().endswith("__syncwarp();"), m[1]
+
+
+def test_inputs_are_read_coherently(source):
+    """The kernels may be on the GPU while the one before them in the stream still writes what they are going to read.  A
+    const __restrict__ pointer promises that nobody does, and allows loads through the read-only path or ahead of the wait."""
+    kernels = re.findall(r"__global__ void\s+__launch_bounds__\((?:[^()]|\([^()]*\))*\)\s*(k_\w+)\(([^)]*)\)", source)
+    assert len(kernels) == source.count("__global__") == 5
+    for name, arguments in kernels:
+        assert "__restrict__" not in arguments, name
+    assert not re.search(r"__ldg\b|\.nc\b", source)
