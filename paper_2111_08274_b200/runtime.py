@@ -101,8 +101,10 @@ class Exchange:
             self.messages = torch.zeros((wl.n_devices, binding.hadfl_packed_bytes(wl.n_params)), dtype=torch.uint8,
                                         device=arena.device)
             self.base = arena.w[0, :wl.n_params].clone()
-            self.residual = torch.zeros((wl.n_devices, arena.stride), device=arena.device) if residual else None
-            self.products = torch.zeros((wl.k, wl.k), device=arena.device)
+            self.residual = None
+            if residual:
+                self.residual = torch.zeros((wl.n_devices, arena.stride), dtype=torch.float32, device=arena.device)
+            self.products = torch.zeros((wl.k, wl.k), dtype=torch.float32, device=arena.device)
 
     def synchronise(self, selected, r, to_all=False, versions=None):
         """Round r's partial aggregation (Eq. 5) from the selected devices' messages, and with to_all the global
