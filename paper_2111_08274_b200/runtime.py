@@ -104,12 +104,18 @@ class Exchange:
             self.residual = None
             if residual:
                 self.residual = torch.zeros((wl.n_devices, arena.stride), dtype=torch.float32, device=arena.device)
-            self.products = torch.zeros((wl.k, wl.k), dtype=torch.float32, device=arena.device)
+            # the products of up to all devices' messages
+            self._room = torch.zeros(wl.n_devices * wl.n_devices, dtype=torch.float32, device=arena.device)
+        self.products = self._products_of(wl.k)
+
+    def _products_of(self, m):
+        return self._room[:m * m].view(m, m)
 
     def synchronise(self, selected, r, to_all=False, versions=None):
-        """Round r's partial aggregation (Eq. 5) from the selected devices' messages, and with to_all the global
-        synchronisation: an overwrite moves the base to the aggregate; a mix (the workload's sync_beta below 1) leaves
-        the devices with different models, and the base as it is."""
+        """Round r's partial aggregation (Eq. 5) from the selected devices' messages (any number of distinct ones; `products`
+        becomes the matrix of theirs), and with to_all the global synchronisation: an overwrite moves the base to the
+        aggregate; a mix (the workload's sync_beta below 1) leaves the devices with different models, and the base as it
+        is."""
         h, wl, messages, base = self.arena.h, self.arena.wl, self.messages.data_ptr(), self.base.data_ptr()
         h.pack(selected, messages, base_ptr=base, residual_ptr=None if self.residual is None else self.residual.data_ptr(),
                rounding=self.rounding, round_=r)
@@ -118,9 +124,10 @@ class Exchange:
                            move_base=overwrite, versions=versions)
         if to_all and not overwrite:
             h.integrate(int(selected[0]), np.setdiff1d(self.arena.ids, selected).astype(np.int32), wl.sync_beta)
+        self.products = self._products_of(len(selected))
         h.packed_dots(selected, messages, self.products.data_ptr())
 
     def read_products(self):
-        """Scalar products of the last messages, [k, k] in draw order (synchronises)."""
+        """Scalar products of the last messages, [m, m] for m selected devices in their order (synchronises)."""
         self.arena.stream.synchronize()
         return self.products.cpu().numpy()

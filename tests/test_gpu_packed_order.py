@@ -54,3 +54,21 @@ def test_calls_one_after_the_other(n, p, storage, rounding):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
     # (an update may be 0 throughout: the base moves to what two devices have, and local steps come every tenth round)
     assert bool(torch.all(torch.isfinite(want[0].float()))) and bool(torch.all(torch.diagonal(want[5], dim1=1, dim2=2) >= 0))
+
+
+@pytest.mark.parametrize("selected", [[2, 0, 1, 4, 3], [4, 1, 3], [0]])
+def test_products_of_an_exchange_with_more_or_fewer_devices_than_the_workload_selects(selected):
+    import packed_reference as ref
+    from paper_2111_08274_b200 import runtime, workloads
+    wl = workloads.Workload("products", 5, 1003, 2, 3, "uniform", steps_lo=1, steps_hi=3, grad_std=1e-2, seed=19)
+    arena = runtime.Arena(wl)
+    exchange = runtime.Exchange(arena, binding.ROUND_NEAREST)
+    arena.h.local_step(arena.ids, wl.steps_for_round(0), wl.lr)
+    exchange.synchronise(selected, 0)
+    got = exchange.read_products()
+    d = np.stack([ref.values(*ref.from_bytes(exchange.messages[i].cpu().numpy(), 1003), 1003) for i in selected])
+    # one sum of 1003 products in fp32: 16 steps of 64 products, 2^-23 each at most, and as much within a step's 64 products
+    assert got.shape == (len(selected),) * 2 and np.all(np.diag(got) > 0)
+    assert np.all(np.abs(got - d @ d.T) <= (16 + 64) * 2.0**-23 * (np.abs(d) @ np.abs(d).T))
+    arena.h.debug_check()
+    arena.close()
