@@ -455,7 +455,8 @@ int hadfl_predict_version(const double *series, int32_t n_obs, double alpha, dou
  * hadfl_synchronize) then returns HADFL_ERR_STATE.  It stands in for a memory checker.  One GPU
  * per process; slower (a table lookup per access; hadfl_init, hadfl_destroy, hadfl_stats_noalloc and the first
  * call of hadfl_pack and its siblings with a buffer synchronise the device, so that such a call is to be made once
- * before it is captured).  Results are identical to the normal build. */
+ * before it is captured).  The buffers of such a call are in the table until the handle is destroyed, a later call's
+ * buffer overlaps them or 16 others have been used since.  Results are identical to the normal build. */
 
 /* 1 in the debug build, 0 otherwise. */
 int hadfl_debug_build(void);

@@ -13,8 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhadfl.so")
 LIB_DEBUG = os.path.join(HERE, "libhadfl_debug.so")   # -DHADFL_DEBUG: bounds-checked kernels
 SOURCES = ["hadfl.cu", "packed.cu", "selection.cpp"]
-DEPS = SOURCES + ["kernels.cuh", "storage.cuh", "packed.cuh", "packed.h", "philox.cuh", "debug_check.cuh", "selection.h",
-                  os.path.join("..", "..", "include", "hadfl.h")]
+DEPS = SOURCES + ["kernels.cuh", "storage.cuh", "packed.cuh", "packed.h", "philox.cuh", "debug_check.cuh", "debug_kept.h",
+                  "selection.h", os.path.join("..", "..", "include", "hadfl.h")]
 
 
 def nvcc_path() -> str:

@@ -12,6 +12,7 @@
 #include <type_traits>
 #include <vector>
 
+#include "debug_kept.h"
 #include "kernels.cuh"
 #include "packed.h"
 #include "selection.h"
@@ -174,43 +175,30 @@ RowStep row_step(const hadfl_handle *h, int dev, uint64_t base, int steps) {
 #ifdef HADFL_DEBUG
 DebugRanges g_debug_host;
 
-// Buffers that callers hand to a call, which may still run when it returns, and again in a captured graph: they stay
-// in the table behind the handles' ranges; the one that was not used for the longest time makes room.
-struct DebugKept {
-  uint64_t lo, hi, used;
-};
-constexpr int kDebugKept = 16;
-DebugKept g_debug_kept[kDebugKept];
+DebugKept g_debug_kept;  // buffers of the callers, behind the handles' ranges
 
 int debug_publish() {
   DebugRanges t = g_debug_host;
-  for (const DebugKept &k : g_debug_kept) {
-    if (!k.used || t.n >= kDebugRanges) continue;
-    t.lo[t.n] = k.lo;
-    t.hi[t.n] = k.hi;
+  g_debug_kept.each([&](const DebugKept::Range &r) {
+    if (t.n >= kDebugRanges) return;
+    t.lo[t.n] = r.lo;
+    t.hi[t.n] = r.hi;
     ++t.n;
-  }
+  });
   const size_t bytes = offsetof(DebugRanges, error);
   return cudaMemcpyToSymbol(g_debug, &t, bytes) == cudaSuccess ? packed_debug_publish(&t, bytes) : 1;
 }
-int debug_keep(const void *p, size_t nbytes) {
-  static uint64_t now = 0;
-  const uint64_t at = (uint64_t)(uintptr_t)p;
-  ++now;
-  DebugKept *oldest = g_debug_kept;
-  for (DebugKept &k : g_debug_kept) {
-    if (k.used && range_holds(k.lo, k.hi, at, nbytes)) {
-      k.used = now;
-      return 0;
-    }
-    if (k.used < oldest->used) oldest = &k;
-  }
-  *oldest = DebugKept{at, at + nbytes, now};
+// The buffers of one call.
+int debug_keep(const void *owner, const DebugKept::Range *call, int n) {
+  if (!g_debug_kept.keep(owner, call, n)) return 0;
   cudaDeviceSynchronize();
   return debug_publish();
 }
+DebugKept::Range debug_range(const void *p, size_t nbytes) {
+  return DebugKept::Range{(uint64_t)(uintptr_t)p, (uint64_t)(uintptr_t)p + nbytes};
+}
 void debug_add(const void *p, size_t nbytes) {
-  if (!p || nbytes == 0 || g_debug_host.n >= kDebugRanges - kDebugKept) return;
+  if (!p || nbytes == 0 || g_debug_host.n >= kDebugRanges - DebugKept::kRoom) return;
   g_debug_host.lo[g_debug_host.n] = (uint64_t)(uintptr_t)p;
   g_debug_host.hi[g_debug_host.n] = (uint64_t)(uintptr_t)p + nbytes;
   ++g_debug_host.n;
@@ -927,6 +915,7 @@ int hadfl_destroy(hadfl_handle *h) {
   debug_remove(h->d_round_partials);
   debug_remove(h->d_round_group_partials);
   debug_remove(h->d_dots);
+  g_debug_kept.forget(h);
   debug_publish();
 #endif
   if (h->own_arena) {
@@ -1163,10 +1152,10 @@ bool exchange_buffers(const hadfl_handle *h, const void *base, const void *resid
 #ifdef HADFL_DEBUG
 int keep_exchange_buffers(const hadfl_handle *h, const void *base, const void *residual, const void *messages) {
   const size_t n = (size_t)h->cfg.n_devices;
-  int bad = debug_keep(messages, n * (size_t)packed_bytes(h->cfg.n_params));
-  if (base) bad |= debug_keep(base, (size_t)h->cfg.n_params * elem_size(h));
-  if (residual) bad |= debug_keep(residual, n * (size_t)h->stride * sizeof(float));
-  return bad;
+  const DebugKept::Range call[] = {debug_range(messages, n * (size_t)packed_bytes(h->cfg.n_params)),
+                                   debug_range(base, base ? (size_t)h->cfg.n_params * elem_size(h) : 0),
+                                   debug_range(residual, residual ? n * (size_t)h->stride * sizeof(float) : 0)};
+  return debug_keep(h, call, 3);
 }
 #define HADFL_KEEP(...)                                             \
   do {                                                              \
@@ -1271,10 +1260,9 @@ int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const vo
   if (o.meets(ByteRange(h->w, (size_t)N * (size_t)h->stride * elem_size(h))) ||
       o.meets(ByteRange(h->m, (size_t)N * (size_t)h->stride * m_elem_size(h))))
     return HADFL_ERR_INVALID;
-  HADFL_KEEP(h, nullptr, nullptr, a_messages);
-  HADFL_KEEP(h, nullptr, nullptr, b_messages);
 #ifdef HADFL_DEBUG
-  if (debug_keep(out, out_bytes)) return HADFL_ERR_CUDA;
+  const DebugKept::Range call[] = {debug_range(a_messages, bytes), debug_range(b_messages, bytes), debug_range(out, out_bytes)};
+  if (debug_keep(h, call, 3)) return HADFL_ERR_CUDA;
 #endif
   HADFL_CUDA(h, launch_packed_dots(packed_shape(h), packed_rows(a_ids, m), (const uint8_t *)a_messages,
                                    packed_rows(b_ids, n), (const uint8_t *)b_messages, out, h->d_dots, h->dots_smem));
