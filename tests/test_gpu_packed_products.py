@@ -115,6 +115,14 @@ def test_two_sets_of_dense_messages(m, n, tiles):
     check(s, a, rng.permutation(rows)[:m], b, rng.integers(0, rows, n))
 
 
+@pytest.mark.parametrize("m,n,shift", [(6, 6, 0), (6, 6, 3), (4, 6, 1), (6, 2, 5)])
+def test_two_sets_that_share_messages(m, n, shift):
+    """The same messages in another order, and two windows of one buffer: each set has its own ids."""
+    s = Long(6, 50_021)
+    both = torch.cat([s.messages(m, True, SMALL), s.messages(n, True, SMALL)])
+    check(s, both[:6], list(range(m)), both[shift:shift + 6], list(range(n))[::-1])
+
+
 @pytest.mark.parametrize("two", [False, True])
 def test_sums_that_fp32_could_not_hold(two):
     """Nearly all values 3 or 6, of one sign: after some 460 tiles of an accumulator a sum that stayed in fp32 would be beyond
