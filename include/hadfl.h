@@ -316,9 +316,10 @@ int hadfl_aggregate_packed(hadfl_handle *h, const int32_t *selected, int32_t k, 
  * = NULL (n = 0): the second set is the first, and out the m x m matrix of its products, which gives the norm of
  * every update and the angle and distance of every two (hadfl_stats: the distances to one replica).
  * out: DEVICE pointer to floats, 4-byte aligned.  A message with a block that reads as NaN has NaN products.
- * Products of single parameters and their sums over up to 2^14 of them are fp32 (and overflow as such), the sums
- * of those have 64 bits.  Deterministic: fixed grid and summation order.  The partial sums lie in memory of the
- * handle: graphs that hold this call of one handle are not to run at the same time. */
+ * Products of single parameters and their sums over up to 2^14 of them are fp32 (and overflow and underflow as
+ * such), the sums of those have 64 bits.  Deterministic: fixed grid and summation order.  The partial sums lie in memory of the
+ * handle: a graph that holds this call is not to run at the same time as another one, or another such call, of the
+ * same handle. */
 int hadfl_packed_dots(hadfl_handle *h, const int32_t *a_ids, int32_t m, const void *a_messages, const int32_t *b_ids,
                       int32_t n, const void *b_messages, float *out);
 

@@ -188,14 +188,16 @@ struct PackParams {
 // works on one (with a residual, whose loads are twice as many bytes, other blocks do for that: 92 us instead of 111 for 4 of
 // 11.2 M fp32 parameters with stochastic rounding, which then has room for more blocks).
 //
-// Bound by HBM, except with stochastic rounding and no residual, where the generator's instructions bind (18 per
-// parameter against 8.5 with rounding to nearest).  Measured, us, and of the copy bandwidth (of what has to be read and
-// written): 4 of 11.2 M fp32, base, residual, stochastic 92 (100 %); 16 of 14.7 M bf16, base, nearest 105 (91 %), stochastic
-// 172 (56 %); 4 of 2^27 fp32 alone 345 (108 %).
+// Bound by HBM, except with stochastic rounding and no residual, where the instructions bind (bf16: 18.6 per parameter,
+// most of them the generator's, against 9.9 with rounding to nearest).  Measured, us, and of the copy bandwidth (of what has
+// to be read and written): 4 of 11.2 M fp32, base, residual, stochastic 90 (102 %); 16 of 14.7 M bf16, base, nearest 105 (91 %),
+// stochastic 174 (55 %; 72 % of the issue slots used); 4 of 2^27 fp32 alone 342 (109 %).
 // Blocks per SM that the compiler is to leave registers for (0: it chooses, mostly few registers and many blocks).  Measured, us,
 // packed and read, the compiler's choice / this one: bf16 without a residual, to nearest, 5 blocks with 48 registers
 // instead of 64: 16 of 14.7 M 207 / 202; with a residual 4 blocks, whose loads then go out together: 8 of 2 M fp32 51.5 / 47.4, 8
-// of 8.4 M 181 / 180.  The others lose with fewer blocks (4 of 2^27 fp32 727; left to one block 780, to five 746).
+// of 8.4 M 181 / 180.  Of the others, fp32 without a residual loses with fewer blocks (4 of 2^27 727; left to one block 780, to
+// five 746); bf16 with stochastic rounding has not been measured with any other number (with a base it takes 71 registers,
+// which are three blocks).
 template <typename WT, bool kResidual, bool kStochastic>
 constexpr int pack_min_blocks() {
   if (kResidual) return 4;
